@@ -52,6 +52,8 @@ extern "C" {
 #define ELIS_DEV_LONG_SEQ    4u  /* a sequence longer than max_seqlen               */
 #define ELIS_DEV_BAD_SLOT    8u  /* a job-table slot outside [0, max_jobs), or a negative token count */
 #define ELIS_DEV_PACK_SIZE  16u  /* packed lengths disagree with the host's total / max, or a job is empty */
+#define ELIS_DEV_NO_PAGES   32u  /* the page pool had too few free pages for every job of a call */
+#define ELIS_DEV_BAD_PAGE   64u  /* a page id or a token's slot outside the cache */
 
 /* ------------------------------------------------------------------ model */
 #define ELIS_POOL_CLS  0 /* the first token's final hidden vector (Sec. 3.2)              */
@@ -385,6 +387,168 @@ int elis_pool_head(const elis_weights *w, const float *hidden, const int32_t *cu
                    int32_t total_tokens, int32_t max_seqlen, float *out_pred, void *workspace, size_t ws_bytes,
                    void *stream);
 
+/* ------------------------------------------------------------------ what the selected batch needs
+ * The served model's memory and attention for the jobs that a round has
+ * selected (Alg. 1: the batch runs one window), and the logits they answer
+ * with: pages of a KV cache handed out on the device from the jobs' lengths,
+ * keys and values kept in 4 bits, attention of the new tokens over them, and
+ * adjusted logits. Same conventions as above: the caller owns every buffer,
+ * calls enqueue only, nothing is allocated; content errors set ELIS_DEV_* bits
+ * that stay until the matching init call and are read with elis_read_status
+ * on the pool's `state` or the cache's `base`. After a content error the
+ * outputs of the entries concerned are undefined; no access leaves the
+ * buffers, and the other entries are served. Every call can be captured into
+ * a HIP graph.
+ */
+
+/*
+ * A pool of n_pages pages of page_tokens tokens each. All arrays are device
+ * memory of the caller, and may be read (not written) between calls:
+ *   state       int32 [2]: ELIS_DEV_* bits, number of free pages
+ *   free_pages  int32 [n_pages]: a stack; the next page handed out is
+ *               free_pages[state[1] - 1]
+ *   held        int32 [max_jobs]: pages that each job slot holds
+ *   table       int32 [max_jobs, max_pages]: their ids, in token order (entries
+ *               past held are meaningless)
+ *   scratch     int32 [4 * max_jobs + 4]: the calls' own
+ * page_tokens is a power of two in [16, 1024]; n_pages * page_tokens,
+ * n_pages and max_jobs * max_pages are below 2^31. Calls on one pool must be
+ * ordered by the caller.
+ */
+typedef struct {
+    int32_t *state, *free_pages, *held, *table, *scratch;
+    int32_t n_pages, page_tokens, max_jobs, max_pages;
+} elis_page_pool;
+
+/* No job holds a page, every page is free (page 0 is handed out first), status cleared. */
+int elis_pages_init(const elis_page_pool *p, void *stream);
+
+/*
+ * Block tables and slot maps of a step: job slots[i] (device int32 [n], n <=
+ * max_jobs) gets the pages that a length of lens[i] tokens (device int32 [n])
+ * needs and it does not hold yet. Jobs are served in the order of the call: if
+ * the free pages do not reach, the first job that they do not reach for and
+ * every later one that needs a page get none (ELIS_DEV_NO_PAGES). A job longer
+ * than max_pages pages gets none (ELIS_DEV_LONG_SEQ). Serving a call again is
+ * harmless: jobs that hold enough keep what they hold. No slot may be named
+ * twice (ELIS_DEV_BAD_SLOT; one of the entries is served).
+ *  cu_new        int32 [n + 1], cu_new[0] = 0, cu_new[n] = total_new: job i's
+ *                last cu_new[i+1] - cu_new[i] tokens are this step's new ones.
+ *  out_slot_map  int32 [total_new] or NULL (then cu_new is not read): the cache
+ *                slot, page * page_tokens + offset, of every new token, or -1
+ *                where the job holds no page for it.
+ *  out_blocks    int32 [n, width] or NULL: the page ids of job i, -1 past them.
+ */
+int elis_pages_grow(const elis_page_pool *p, const int32_t *slots, const int32_t *lens, const int32_t *cu_new,
+                    int32_t n, int32_t total_new, int32_t width, int32_t *out_blocks, int32_t *out_slot_map,
+                    void *stream);
+
+/*
+ * Pages given back: job slots[i] keeps the pages of its first lens[i] tokens
+ * (0: none, a job that has finished or was preempted). A trim to the former
+ * lengths undoes a grow exactly, the order of the free pages included.
+ */
+int elis_pages_trim(const elis_page_pool *p, const int32_t *slots, const int32_t *lens, int32_t n, void *stream);
+
+/*
+ * One layer's keys and values in 4 bits. `base` is 256-byte aligned device
+ * memory of elis_kv_cache_bytes(): a header of 256 bytes (the status word
+ * first), then n_pages pages, each [n_kv_heads][page_tokens / 16] records of 17
+ * * d_head bytes that hold 16 tokens of one head:
+ *   keys    [16][d_head / 2]       two E2M1 values a byte, the lower value in the low half
+ *   values  [4][16][4][d_head/32]  token 4a + b, values (d_head/16) c ... of column c at [a][c][b]
+ *   scales  E8M0 (2^(byte - 127)), one for 32 values: keys [16][d_head/32], values [4][d_head/32][4]
+ * A scale is the least power of two 2^e with max|x| < 7 * 2^e, e clamped to
+ * [-125, 125]; a value is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it
+ * (ties to the even code, above 6 saturating). 32 values of which one is
+ * infinite or NaN get the scale byte 255 and read as NaN.
+ * Supported: d_head 64 and 128, n_kv_heads <= 1024, pages as elis_page_pool.
+ */
+typedef struct {
+    void *base;
+    int32_t n_pages, page_tokens, n_kv_heads, d_head;
+} elis_kv_cache;
+
+/* Bytes of the cache (0 if the sizes are not supported). */
+size_t elis_kv_cache_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t d_head);
+
+/* Status cleared; the pages are left as they are (only slots that were appended to may be read). */
+int elis_kv_init(const elis_kv_cache *c, void *stream);
+
+/*
+ * Keys and values of n_tokens new tokens into the slots of slot_map (device
+ * int32 [n_tokens]; -1: the token is not kept). k, v: bf16, token t's row at t *
+ * stride elements, head h at h * d_head in it (rows may be part of a wider
+ * matrix: strides of at least n_kv_heads * d_head). 16-byte aligned rows load
+ * widest; others are served too. No slot may be named twice.
+ */
+int elis_kv_append(const elis_kv_cache *c, const uint16_t *k, const uint16_t *v, int64_t k_stride, int64_t v_stride,
+                   const int32_t *slot_map, int32_t n_tokens, void *stream);
+
+/* What the cache keeps of the tokens in slot_map, as bf16 (exact; zeros for slot -1). Layout as elis_kv_append. */
+int elis_kv_read(const elis_kv_cache *c, const int32_t *slot_map, int32_t n_tokens, uint16_t *out_k, uint16_t *out_v,
+                 int64_t k_stride, int64_t v_stride, void *stream);
+
+/* Bytes of workspace elis_kv_attention needs for these sizes (0 if they are invalid). */
+size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t d_head);
+
+/*
+ * Causal attention of every request's new tokens over its cached keys, its own
+ * among them (append first). Request i has the query rows cu_q[i] .. cu_q[i+1]-1
+ * and kv_lens[i] cached tokens; its query t stands at position p = kv_lens[i] -
+ * q_len + t and sees the keys j <= p, with window > 0 only those with j > p -
+ * window. Query head h reads kv head h / (n_heads / n_kv_heads):
+ *     out = sum_j softmax_j(scale * q . k_j) v_j, zeros for a query that sees no key.
+ *  q, out      bf16, row t at t * stride elements, head h at h * d_head in it.
+ *  cu_q        int32 [n + 1], 0 = cu_q[0] <= ... <= cu_q[n] <= total_q (rows past cu_q[n] are left as they are).
+ *  max_q       host: at least every q_len.   max_kv  host: at least every kv_lens[i].
+ *  blocks      int32 [block_rows, blocks_stride]: page ids in token order; request i's row is
+ *              rows[i] (device int32 [n]; with a pool's table and slots no copy is needed), or i if rows is NULL.
+ *              A key on an id outside the cache is not seen (ELIS_DEV_BAD_PAGE).
+ *  kv_lens     int32 [n].   scale > 0.
+ *  workspace   256-byte aligned, elis_kv_attention_workspace_bytes() bytes.
+ * Products of bf16 operands (the keys and values are exact in bf16, the weights
+ * are rounded once) with fp32 sums and statistics. n <= 65535; max_kv <=
+ * blocks_stride * page_tokens (else ELIS_ESHAPE).
+ */
+int elis_kv_attention(const elis_kv_cache *c, const uint16_t *q, int64_t q_stride, const int32_t *cu_q, int32_t n,
+                      int32_t total_q, int32_t max_q, const int32_t *blocks, int32_t block_rows, int32_t blocks_stride,
+                      const int32_t *rows, const int32_t *kv_lens, int32_t max_kv, int32_t n_heads, float scale,
+                      int32_t window, uint16_t *out, int64_t out_stride, void *workspace, size_t ws_bytes,
+                      void *stream);
+
+#define ELIS_DT_F32  0
+#define ELIS_DT_BF16 1
+
+/*
+ * Logits of n rows (one for each job of the batch) made ready for sampling.
+ * Row i's history is token_ids[cu_seqlens[i] .. cu_seqlens[i+1]-1], in the
+ * packed form that elis_jobs_pack writes; its first prompt_lens[i] tokens are
+ * the prompt. With h: v occurs in the history, c: how often past the prompt,
+ *     y = h ? (x > 0 ? x / repetition : x * repetition) : x
+ *     y = y - frequency * c - (c > 0 ? presence : 0)
+ *     y = y + (the row's biases of token v, added up in list order)
+ *     y = -inf where the row's mask has bit v clear
+ * in fp32, written to out (which may be the logits themselves if they are
+ * fp32 and the strides are equal).
+ *  logits       ELIS_DT_F32 or ELIS_DT_BF16 [n, vocab], row i at i * in_stride elements; out at i * out_stride.
+ *  token_ids    int32 [total_tokens] or NULL (no history; then cu_seqlens and prompt_lens are not read).
+ *               Ids outside [0, vocab) are passed over; ranges are cut to [0, total_tokens).
+ *  prompt_lens  int32 [n] or NULL (no prompts: everything counts).
+ *  repetition, frequency, presence   fp32 [n] each, or NULL (1, 0, 0).
+ *  bias_cu      int32 [n + 1] or NULL: row i's biases are bias_tokens / bias_values[bias_cu[i] .. bias_cu[i+1]-1]
+ *               of the bias_total entries, in any order, tokens more than once allowed.
+ *  mask         uint32 [n_masks, mask_stride words] or NULL: bit v % 32 of word v / 32 allows token v.
+ *  mask_rows    int32 [n] or NULL (row i): the row's mask; one outside [0, n_masks) means none.
+ */
+int elis_logits_adjust(const void *logits, int32_t dtype, int64_t in_stride, int32_t n, int32_t vocab,
+                       const int32_t *token_ids, const int32_t *cu_seqlens, int32_t total_tokens,
+                       const int32_t *prompt_lens, const float *repetition, const float *frequency,
+                       const float *presence, const int32_t *bias_cu, const int32_t *bias_tokens,
+                       const float *bias_values, int32_t bias_total, const uint32_t *mask, int32_t n_masks,
+                       int64_t mask_stride, const int32_t *mask_rows, float *out, int64_t out_stride, void *stream);
+
 /* ------------------------------------------------------------------ timing (opt-in)
  * When a class is enabled, each timed launch of it enqueues its kernels with
  * a start/stop HIP event pair attached to each dispatch (hipExtLaunchKernel),
@@ -408,7 +572,11 @@ int elis_pool_head(const elis_weights *w, const float *hidden, const int32_t *cu
 #define ELIS_K_POOL_HEAD 8
 #define ELIS_K_SELECT    9
 #define ELIS_K_JOBS      10 /* job-table append / pack / store / gather */
-#define ELIS_K_COUNT     11
+#define ELIS_K_PAGES     11
+#define ELIS_K_KV        12 /* 4-bit cache: init / append / read */
+#define ELIS_K_KV_ATTENTION 13
+#define ELIS_K_LOGITS    14
+#define ELIS_K_COUNT     15
 
 int elis_timing_enable(uint32_t class_mask); /* bit c enables class c; 0 disables */
 int elis_timing_stride(int32_t every);       /* every >= 1, else ELIS_EINVAL */

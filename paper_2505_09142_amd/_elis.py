@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libelis.so")
 
@@ -27,6 +27,8 @@ ELIS_DEV_BAD_CU = 2
 ELIS_DEV_LONG_SEQ = 4
 ELIS_DEV_BAD_SLOT = 8
 ELIS_DEV_PACK_SIZE = 16
+ELIS_DEV_NO_PAGES = 32
+ELIS_DEV_BAD_PAGE = 64
 
 ELIS_POOL_CLS = 0
 ELIS_POOL_MEAN = 1
@@ -36,9 +38,11 @@ ELIS_ACT_IDENTITY = 1
 ELIS_EPI_BIAS_BF16 = 0
 ELIS_EPI_BIAS_GELU_BF16 = 1
 ELIS_EPI_BIAS_RES_F32 = 2
+ELIS_DT_F32 = 0
+ELIS_DT_BF16 = 1
 
 KERNEL_CLASSES = ("seqmap", "embed_ln", "gemm_qkv", "attention", "gemm_o", "layernorm", "gemm_ffn1",
-                  "gemm_ffn2", "pool_head", "select", "jobs")
+                  "gemm_ffn2", "pool_head", "select", "jobs", "pages", "kv", "kv_attention", "logits")
 K = {name: i for i, name in enumerate(KERNEL_CLASSES)}
 
 
@@ -73,6 +77,15 @@ class elis_weights(ctypes.Structure):
 
 class elis_job_table(ctypes.Structure):
     _fields_ = [("base", c_void_p), ("max_jobs", c_int32), ("max_pos", c_int32)]
+
+
+class elis_page_pool(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("state", "free_pages", "held", "table", "scratch")] + \
+               [(n, c_int32) for n in ("n_pages", "page_tokens", "max_jobs", "max_pages")]
+
+
+class elis_kv_cache(ctypes.Structure):
+    _fields_ = [("base", c_void_p)] + [(n, c_int32) for n in ("n_pages", "page_tokens", "n_kv_heads", "d_head")]
 
 
 # name -> (restype, argtypes); mirrors include/elis.h
@@ -115,6 +128,23 @@ SIGNATURES = {
                                  c_void_p, c_size_t, c_void_p]),
     "elis_jobs_select_aged": (c_int, [POINTER(elis_job_table), c_void_p, c_void_p, c_float, c_int32, c_int32,
                                       c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "elis_pages_init": (c_int, [POINTER(elis_page_pool), c_void_p]),
+    "elis_pages_grow": (c_int, [POINTER(elis_page_pool), c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                c_void_p, c_void_p, c_void_p]),
+    "elis_pages_trim": (c_int, [POINTER(elis_page_pool), c_void_p, c_void_p, c_int32, c_void_p]),
+    "elis_kv_cache_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32]),
+    "elis_kv_init": (c_int, [POINTER(elis_kv_cache), c_void_p]),
+    "elis_kv_append": (c_int, [POINTER(elis_kv_cache), c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int32,
+                               c_void_p]),
+    "elis_kv_read": (c_int, [POINTER(elis_kv_cache), c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int64,
+                             c_void_p]),
+    "elis_kv_attention_workspace_bytes": (c_size_t, [c_int32] * 7),
+    "elis_kv_attention": (c_int, [POINTER(elis_kv_cache), c_void_p, c_int64, c_void_p, c_int32, c_int32, c_int32,
+                                  c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_float, c_int32,
+                                  c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
+    "elis_logits_adjust": (c_int, [c_void_p, c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
+                                   c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                   c_int32, c_int64, c_void_p, c_void_p, c_int64, c_void_p]),
     "elis_timing_enable": (c_int, [c_uint32]),
     "elis_timing_stride": (c_int, [c_int32]),
     "elis_timing_reset": (c_int, []),
@@ -278,6 +308,61 @@ def elis_jobs_select_aged(t: elis_job_table, slots: int, wait: int, aging: float
                           stream: int | None) -> int:
     return lib().elis_jobs_select_aged(_tab(t), slots, wait, aging, a, batch_cap, out_slots, out_count, workspace,
                                        ws_bytes, stream)
+
+
+def elis_pages_init(p: elis_page_pool, stream: int | None) -> int:
+    return lib().elis_pages_init(_tab(p), stream)
+
+
+def elis_pages_grow(p: elis_page_pool, slots: int, lens: int, cu_new: int | None, n: int, total_new: int, width: int,
+                    out_blocks: int | None, out_slot_map: int | None, stream: int | None) -> int:
+    return lib().elis_pages_grow(_tab(p), slots, lens, cu_new, n, total_new, width, out_blocks, out_slot_map, stream)
+
+
+def elis_pages_trim(p: elis_page_pool, slots: int, lens: int, n: int, stream: int | None) -> int:
+    return lib().elis_pages_trim(_tab(p), slots, lens, n, stream)
+
+
+def elis_kv_cache_bytes(n_pages: int, page_tokens: int, n_kv_heads: int, d_head: int) -> int:
+    return lib().elis_kv_cache_bytes(n_pages, page_tokens, n_kv_heads, d_head)
+
+
+def elis_kv_init(c: elis_kv_cache, stream: int | None) -> int:
+    return lib().elis_kv_init(_tab(c), stream)
+
+
+def elis_kv_append(c: elis_kv_cache, k: int, v: int, k_stride: int, v_stride: int, slot_map: int, n_tokens: int,
+                   stream: int | None) -> int:
+    return lib().elis_kv_append(_tab(c), k, v, k_stride, v_stride, slot_map, n_tokens, stream)
+
+
+def elis_kv_read(c: elis_kv_cache, slot_map: int, n_tokens: int, out_k: int, out_v: int, k_stride: int, v_stride: int,
+                 stream: int | None) -> int:
+    return lib().elis_kv_read(_tab(c), slot_map, n_tokens, out_k, out_v, k_stride, v_stride, stream)
+
+
+def elis_kv_attention_workspace_bytes(n: int, total_q: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int,
+                                      d_head: int) -> int:
+    return lib().elis_kv_attention_workspace_bytes(n, total_q, max_q, max_kv, n_heads, n_kv_heads, d_head)
+
+
+def elis_kv_attention(c: elis_kv_cache, q: int, q_stride: int, cu_q: int, n: int, total_q: int, max_q: int, blocks: int,
+                      block_rows: int, blocks_stride: int, rows: int | None, kv_lens: int, max_kv: int, n_heads: int,
+                      scale: float, window: int, out: int, out_stride: int, workspace: int, ws_bytes: int,
+                      stream: int | None) -> int:
+    return lib().elis_kv_attention(_tab(c), q, q_stride, cu_q, n, total_q, max_q, blocks, block_rows, blocks_stride,
+                                   rows, kv_lens, max_kv, n_heads, scale, window, out, out_stride, workspace, ws_bytes,
+                                   stream)
+
+
+def elis_logits_adjust(logits: int, dtype: int, in_stride: int, n: int, vocab: int, token_ids: int | None,
+                       cu_seqlens: int | None, total_tokens: int, prompt_lens: int | None, repetition: int | None,
+                       frequency: int | None, presence: int | None, bias_cu: int | None, bias_tokens: int | None,
+                       bias_values: int | None, bias_total: int, mask: int | None, n_masks: int, mask_stride: int,
+                       mask_rows: int | None, out: int, out_stride: int, stream: int | None) -> int:
+    return lib().elis_logits_adjust(logits, dtype, in_stride, n, vocab, token_ids, cu_seqlens, total_tokens,
+                                    prompt_lens, repetition, frequency, presence, bias_cu, bias_tokens, bias_values,
+                                    bias_total, mask, n_masks, mask_stride, mask_rows, out, out_stride, stream)
 
 
 def elis_timing_enable(class_mask: int) -> int:

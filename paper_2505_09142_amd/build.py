@@ -38,8 +38,10 @@ CFLAGS = [
 # Its kernel arguments, and the product kernels', are preloaded into SGPRs at wave launch (the
 # attention work-group's first scalar load is then its work-list entry: 52.5 -> 51.9 us per
 # BERT-base layer; the products gain ~0.5 us per launch).
+# kv_attention.hip keeps its accumulators in VGPRs for the same reason; its cache may hold NaN, so it honours them.
 EXTRA = {
     "attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans", "-mllvm", "-amdgpu-kernarg-preload-count=16"],
+    "kv_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "gemm.hip": ["-mllvm", "-amdgpu-kernarg-preload-count=16"],
 }
 

@@ -684,6 +684,233 @@ int elis_layernorm(const float* x, const float* g, const float* b, int32_t rows,
               [&] { return launch_layernorm(x, g, b, rows, d, eps, LnOut{out_f32, out_bf16, nullptr, nullptr}, st); }));
 }
 
+namespace {
+
+int log2_of(int v) {  // -1 if v is not a power of two
+    if (v < 1 || (v & (v - 1))) return -1;
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+bool page_size_ok(int32_t n_pages, int32_t page_tokens) {
+    return page_tokens >= 16 && page_tokens <= 1024 && log2_of(page_tokens) > 0 &&
+           static_cast<int64_t>(n_pages) * page_tokens <= INT32_MAX;
+}
+
+int check_pool(const elis_page_pool* p) {
+    if (!p || !p->state || !p->free_pages || !p->held || !p->table || !p->scratch) return ELIS_EINVAL;
+    if (p->n_pages < 1 || p->max_jobs < 1 || p->max_pages < 1) return ELIS_EINVAL;
+    if (!page_size_ok(p->n_pages, p->page_tokens)) return ELIS_EUNSUPPORTED;
+    if (static_cast<int64_t>(p->max_jobs) * p->max_pages > INT32_MAX || p->max_jobs > INT32_MAX / 4 - 4) return ELIS_EUNSUPPORTED;
+    return ELIS_OK;
+}
+
+PagePoolView pool_view(const elis_page_pool* p) {
+    return PagePoolView{p->state, p->free_pages, p->held, p->table, p->scratch,
+                        p->n_pages, p->page_tokens, log2_of(p->page_tokens), p->max_jobs, p->max_pages};
+}
+
+int check_cache_sizes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t d_head) {
+    if (n_pages < 1 || n_kv_heads < 1 || d_head < 1) return ELIS_EINVAL;
+    if (!page_size_ok(n_pages, page_tokens) || n_kv_heads > 1024 || (d_head != 64 && d_head != 128)) return ELIS_EUNSUPPORTED;
+    return ELIS_OK;
+}
+
+constexpr size_t kKvHeader = 256;
+
+int check_cache(const elis_kv_cache* c) {
+    if (!c || !c->base || !aligned(c->base)) return ELIS_EINVAL;
+    return check_cache_sizes(c->n_pages, c->page_tokens, c->n_kv_heads, c->d_head);
+}
+
+KvCacheView cache_view(const elis_kv_cache* c) {
+    return KvCacheView{static_cast<uint32_t*>(c->base), static_cast<uint8_t*>(c->base) + kKvHeader,
+                       c->n_pages, c->page_tokens, log2_of(c->page_tokens), c->n_kv_heads, c->d_head};
+}
+
+// Keys and values of a call: row strides, and a launch that stays below 2^31 threads.
+int check_kv_rows(const elis_kv_cache* c, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                  const int32_t* slot_map, int32_t n_tokens) {
+    if (n_tokens < 0 || (n_tokens > 0 && (!k || !v || !slot_map))) return ELIS_EINVAL;
+    const int64_t row = static_cast<int64_t>(c->n_kv_heads) * c->d_head;
+    if (k_stride < row || v_stride < row) return ELIS_ESHAPE;
+    if ((static_cast<int64_t>(n_tokens) + 3) / 4 * 4 * row / 8 > INT32_MAX) return ELIS_ESHAPE;
+    return ELIS_OK;
+}
+
+int check_kv_attention_sizes(int32_t n, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads, int32_t n_kv_heads,
+                             int32_t d_head) {
+    if (n < 1 || total_q < 0 || max_q < 1 || max_kv < 0 || n_heads < 1 || n_kv_heads < 1 || d_head < 1) return ELIS_EINVAL;
+    if (n_heads % n_kv_heads || n_kv_heads > 1024 || n_heads > 16384 || (d_head != 64 && d_head != 128)) return ELIS_EUNSUPPORTED;
+    if (n > 65535) return ELIS_ESHAPE;
+    // row numbers and launch sizes stay below 2^31
+    if (static_cast<int64_t>(max_q) * (n_heads / n_kv_heads) > INT32_MAX / 128 ||
+        static_cast<int64_t>(total_q) * n_heads > INT32_MAX / 64)
+        return ELIS_ESHAPE;
+    return ELIS_OK;
+}
+
+size_t kv_attention_ws(const KvAttnPlan& p, int32_t d_head) {
+    const size_t parts = p.small_parts + p.many_parts;
+    return kAlign + align_up(parts * d_head * sizeof(float)) + align_up(parts * sizeof(float2));
+}
+
+}  // namespace
+
+int elis_pages_init(const elis_page_pool* p, void* stream) {
+    const int r = check_pool(p);
+    if (r != ELIS_OK) return r;
+    return status_of(timed(ELIS_K_PAGES, [&] { return launch_pages_init(pool_view(p), static_cast<hipStream_t>(stream)); }));
+}
+
+int elis_pages_grow(const elis_page_pool* p, const int32_t* slots, const int32_t* lens, const int32_t* cu_new, int32_t n,
+                    int32_t total_new, int32_t width, int32_t* out_blocks, int32_t* out_slot_map, void* stream) {
+    const int r = check_pool(p);
+    if (r != ELIS_OK) return r;
+    if (n < 0 || total_new < 0 || width < 0) return ELIS_EINVAL;
+    if (n == 0) return ELIS_OK;
+    if (!slots || !lens || (out_slot_map && !cu_new)) return ELIS_EINVAL;
+    if (n > p->max_jobs || (out_blocks && width > p->max_pages)) return ELIS_ESHAPE;
+    int32_t* map = total_new > 0 ? out_slot_map : nullptr;
+    int32_t* blocks = width > 0 ? out_blocks : nullptr;
+    return status_of(timed(ELIS_K_PAGES, [&] {
+        return launch_pages_grow(pool_view(p), slots, lens, cu_new, n, total_new, width, blocks, map, static_cast<hipStream_t>(stream));
+    }));
+}
+
+int elis_pages_trim(const elis_page_pool* p, const int32_t* slots, const int32_t* lens, int32_t n, void* stream) {
+    const int r = check_pool(p);
+    if (r != ELIS_OK) return r;
+    if (n < 0 || (n > 0 && (!slots || !lens))) return ELIS_EINVAL;
+    if (n == 0) return ELIS_OK;
+    if (n > p->max_jobs) return ELIS_ESHAPE;
+    return status_of(timed(ELIS_K_PAGES, [&] { return launch_pages_trim(pool_view(p), slots, lens, n, static_cast<hipStream_t>(stream)); }));
+}
+
+size_t elis_kv_cache_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t d_head) {
+    if (check_cache_sizes(n_pages, page_tokens, n_kv_heads, d_head) != ELIS_OK) return 0;
+    return kKvHeader + static_cast<size_t>(n_pages) * n_kv_heads * (page_tokens / 16) * 17 * d_head;
+}
+
+int elis_kv_init(const elis_kv_cache* c, void* stream) {
+    const int r = check_cache(c);
+    if (r != ELIS_OK) return r;
+    return status_of(timed(ELIS_K_KV, [&] { return launch_kv_init(cache_view(c), static_cast<hipStream_t>(stream)); }));
+}
+
+int elis_kv_append(const elis_kv_cache* c, const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride,
+                   const int32_t* slot_map, int32_t n_tokens, void* stream) {
+    int r = check_cache(c);
+    if (r != ELIS_OK) return r;
+    r = check_kv_rows(c, k, v, k_stride, v_stride, slot_map, n_tokens);
+    if (r != ELIS_OK || n_tokens == 0) return r;
+    return status_of(timed(ELIS_K_KV, [&] {
+        return launch_kv_append(cache_view(c), k, v, k_stride, v_stride, slot_map, n_tokens, static_cast<hipStream_t>(stream));
+    }));
+}
+
+int elis_kv_read(const elis_kv_cache* c, const int32_t* slot_map, int32_t n_tokens, uint16_t* out_k, uint16_t* out_v,
+                 int64_t k_stride, int64_t v_stride, void* stream) {
+    int r = check_cache(c);
+    if (r != ELIS_OK) return r;
+    r = check_kv_rows(c, out_k, out_v, k_stride, v_stride, slot_map, n_tokens);
+    if (r != ELIS_OK || n_tokens == 0) return r;
+    return status_of(timed(ELIS_K_KV, [&] {
+        return launch_kv_read(cache_view(c), slot_map, n_tokens, out_k, out_v, k_stride, v_stride, static_cast<hipStream_t>(stream));
+    }));
+}
+
+size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t d_head) {
+    if (check_kv_attention_sizes(n, total_q, max_q, max_kv, n_heads, n_kv_heads, d_head) != ELIS_OK) return 0;
+    return kv_attention_ws(plan_kv_attention(n, total_q, max_q, max_kv, n_heads, n_kv_heads), d_head);
+}
+
+int elis_kv_attention(const elis_kv_cache* c, const uint16_t* q, int64_t q_stride, const int32_t* cu_q, int32_t n,
+                      int32_t total_q, int32_t max_q, const int32_t* blocks, int32_t block_rows, int32_t blocks_stride,
+                      const int32_t* rows, const int32_t* kv_lens, int32_t max_kv, int32_t n_heads, float scale,
+                      int32_t window, uint16_t* out, int64_t out_stride, void* workspace, size_t ws_bytes, void* stream) {
+    int r = check_cache(c);
+    if (r != ELIS_OK) return r;
+    if (!q || !cu_q || !blocks || !kv_lens || !out || !workspace || !aligned(workspace)) return ELIS_EINVAL;
+    if (!(scale > 0.f) || !isfinite(scale) || window < 0 || block_rows < 1 || blocks_stride < 1) return ELIS_EINVAL;
+    r = check_kv_attention_sizes(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads, c->d_head);
+    if (r != ELIS_OK) return r;
+    const int64_t row = static_cast<int64_t>(n_heads) * c->d_head;
+    if (q_stride < row || out_stride < row || static_cast<int64_t>(blocks_stride) * c->page_tokens < max_kv || (!rows && block_rows < n))
+        return ELIS_ESHAPE;
+    const KvAttnPlan p = plan_kv_attention(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads);
+    if (ws_bytes < kv_attention_ws(p, c->d_head)) return ELIS_EWORKSPACE;
+    if (total_q == 0) return ELIS_OK;
+    KvAttnArgs a{};
+    a.c = cache_view(c);
+    a.q = q;
+    a.q_stride = q_stride;
+    a.q_vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (q_stride & 7) == 0;
+    a.out_vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && (out_stride & 7) == 0;
+    a.cu = cu_q;
+    a.n = n;
+    a.total_q = total_q;
+    a.max_q = max_q;
+    a.blocks = blocks;
+    a.blocks_stride = blocks_stride;
+    a.block_rows = block_rows;
+    a.rows = rows;
+    a.kv_lens = kv_lens;
+    a.max_kv = max_kv;
+    a.n_heads = n_heads;
+    a.group = n_heads / c->n_kv_heads;
+    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.window = window;
+    a.out = out;
+    a.out_stride = out_stride;
+    const size_t parts = p.small_parts + p.many_parts;
+    a.part_o = at<float>(workspace, kAlign);
+    a.part_ml = at<float2>(workspace, kAlign + align_up(parts * c->d_head * sizeof(float)));
+    return status_of(timed(ELIS_K_KV_ATTENTION, [&] { return launch_kv_attention(a, p, static_cast<hipStream_t>(stream)); }));
+}
+
+int elis_logits_adjust(const void* logits, int32_t dtype, int64_t in_stride, int32_t n, int32_t vocab, const int32_t* token_ids,
+                       const int32_t* cu_seqlens, int32_t total_tokens, const int32_t* prompt_lens, const float* repetition,
+                       const float* frequency, const float* presence, const int32_t* bias_cu, const int32_t* bias_tokens,
+                       const float* bias_values, int32_t bias_total, const uint32_t* mask, int32_t n_masks, int64_t mask_stride,
+                       const int32_t* mask_rows, float* out, int64_t out_stride, void* stream) {
+    if (dtype != ELIS_DT_F32 && dtype != ELIS_DT_BF16) return ELIS_EINVAL;
+    if (n < 0 || vocab < 1 || total_tokens < 0 || bias_total < 0) return ELIS_EINVAL;
+    if (n == 0) return ELIS_OK;
+    if (!logits || !out || (token_ids && !cu_seqlens) || (bias_cu && bias_total > 0 && (!bias_tokens || !bias_values))) return ELIS_EINVAL;
+    if (mask && n_masks < 1) return ELIS_EINVAL;
+    if (in_stride < vocab || out_stride < vocab || (mask && mask_stride < (static_cast<int64_t>(vocab) + 31) / 32)) return ELIS_ESHAPE;
+    if (n > 65535 || vocab > (1 << 28)) return ELIS_ESHAPE;
+    if (logits == out && (dtype != ELIS_DT_F32 || in_stride != out_stride)) return ELIS_EINVAL;
+    if (mask && !mask_rows && n_masks < n) return ELIS_ESHAPE;
+    LogitsArgs a{};
+    a.logits = logits;
+    a.bf16 = dtype == ELIS_DT_BF16;
+    a.in_stride = in_stride;
+    a.n = n;
+    a.vocab = vocab;
+    a.token_ids = total_tokens > 0 ? token_ids : nullptr;
+    a.cu = cu_seqlens;
+    a.total_tokens = total_tokens;
+    a.prompt_lens = prompt_lens;
+    a.repetition = repetition;
+    a.frequency = frequency;
+    a.presence = presence;
+    a.bias_cu = bias_total > 0 ? bias_cu : nullptr;
+    a.bias_tokens = bias_tokens;
+    a.bias_values = bias_values;
+    a.bias_total = bias_total;
+    a.mask = mask;
+    a.n_masks = n_masks;
+    a.mask_stride = mask_stride;
+    a.mask_rows = mask_rows;
+    a.out = out;
+    a.out_stride = out_stride;
+    return status_of(timed(ELIS_K_LOGITS, [&] { return launch_logits_adjust(a, static_cast<hipStream_t>(stream)); }));
+}
+
 int elis_linear_plan(int32_t m, int32_t n, int32_t k, int32_t epilogue, int32_t* out) {
     if (!out || m <= 0 || n <= 0 || k <= 0) return ELIS_EINVAL;
     if (epilogue != ELIS_EPI_BIAS_BF16 && epilogue != ELIS_EPI_BIAS_GELU_BF16 && epilogue != ELIS_EPI_BIAS_RES_F32)

@@ -154,6 +154,95 @@ hipError_t launch_jobs_map(const int32_t* slots, const int32_t* idx, const int32
 hipError_t launch_jobs_select(JobTable t, const int32_t* slots, const float* wait, float aging, int a, int k,
                               int32_t* out_slots, int32_t* out_count, void* workspace, hipStream_t st);
 
+// pages.hip: pages of a KV cache handed out to job slots, block tables and slot maps.
+struct PagePoolView {
+    int32_t* state;       // [2]: status bits, free pages
+    int32_t* free_pages;  // [n_pages] stack
+    int32_t* held;        // [max_jobs]
+    int32_t* table;       // [max_jobs, max_pages]
+    int32_t* scratch;     // [4 * max_jobs + 4]
+    int n_pages, page_tokens, page_shift, max_jobs, max_pages;
+};
+hipError_t launch_pages_init(PagePoolView p, hipStream_t st);
+// blocks: [n, width] or null; map: [total] or null (cu is read only with a map).
+hipError_t launch_pages_grow(PagePoolView p, const int32_t* slots, const int32_t* lens, const int32_t* cu, int n, int total, int width,
+                             int32_t* blocks, int32_t* map, hipStream_t st);
+hipError_t launch_pages_trim(PagePoolView p, const int32_t* slots, const int32_t* lens, int n, hipStream_t st);
+
+// kv_cache.hip: the 4-bit paged cache (records in kv_cache.h).
+struct KvCacheView {
+    uint32_t* status;
+    uint8_t* pages;
+    int n_pages, page_tokens, page_shift, n_kv_heads, d_head;
+};
+hipError_t launch_kv_init(KvCacheView c, hipStream_t st);
+// Strides in elements from token to token.
+hipError_t launch_kv_append(KvCacheView c, const uint16_t* k, const uint16_t* v, long long k_stride, long long v_stride, const int32_t* map, int n,
+                            hipStream_t st);
+hipError_t launch_kv_read(KvCacheView c, const int32_t* map, int n, uint16_t* k, uint16_t* v, long long k_stride, long long v_stride, hipStream_t st);
+
+// kv_attention.hip
+// Launches of one call: requests of up to `small` rows (new tokens x heads of a group) in tiles of 16 small_nb rows
+// and chunks of small_chunk keys, longer ones in tiles of their own.
+struct KvAttnPlan {
+    int small, small_nb, small_rows, small_chunk, small_chunks;
+    bool many;
+    int many_chunk, many_chunks;
+    size_t small_parts, many_parts;  // chunk results to join (d_head floats and two more each)
+};
+KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads);
+struct KvAttnArgs {
+    KvCacheView c;
+    const uint16_t* q;
+    long long q_stride;
+    bool q_vec, out_vec;     // 16-byte accesses fit
+    const int32_t* cu;       // [n + 1]
+    int n, total_q, max_q;
+    const int32_t* blocks;   // [block_rows, blocks_stride]
+    long long blocks_stride;
+    int block_rows;
+    const int32_t* rows;     // [n] or null: row i
+    const int32_t* kv_lens;  // [n]
+    int max_kv, n_heads, group;
+    float scale_log2;
+    int window;
+    uint16_t* out;
+    long long out_stride;
+    int nchunks, chunk, small, small_rows;
+    float* part_o;
+    float2* part_ml;
+};
+// Row of the chunk results that (request, kv head, row) or (token, head) has.
+__device__ __forceinline__ size_t part_row(const KvAttnArgs& a, bool many, int req, int h, int tok, int head, int r) {
+    return many ? static_cast<size_t>(tok) * a.n_heads + head
+                : (static_cast<size_t>(req) * a.c.n_kv_heads + h) * a.small_rows + r;
+}
+hipError_t launch_kv_attention(KvAttnArgs a, const KvAttnPlan& p, hipStream_t st);
+
+// logits.hip
+struct LogitsArgs {
+    const void* logits;
+    bool bf16;
+    long long in_stride;
+    int n, vocab;
+    const int32_t* token_ids;   // or null
+    const int32_t* cu;
+    long long total_tokens;
+    const int32_t* prompt_lens;  // or null, as are the next three
+    const float *repetition, *frequency, *presence;
+    const int32_t* bias_cu;     // or null
+    const int32_t* bias_tokens;
+    const float* bias_values;
+    long long bias_total;
+    const uint32_t* mask;       // or null
+    int n_masks;
+    long long mask_stride;
+    const int32_t* mask_rows;   // or null: row i
+    float* out;
+    long long out_stride;
+};
+hipError_t launch_logits_adjust(const LogitsArgs& a, hipStream_t st);
+
 // ------------------------------------------------------------------ launching
 // Timing hook of the opt-in per-class timing (api.hip): while a timed class is
 // being enqueued it hands out one start/stop event pair per kernel launch;
