@@ -510,7 +510,7 @@ size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max
  *  workspace   256-byte aligned, elis_kv_attention_workspace_bytes() bytes.
  * Products of bf16 operands (the keys and values are exact in bf16, the weights
  * are rounded once) with fp32 sums and statistics. n <= 65535; max_kv <=
- * blocks_stride * page_tokens (else ELIS_ESHAPE).
+ * blocks_stride * page_tokens and <= 2^30 (else ELIS_ESHAPE).
  */
 int elis_kv_attention(const elis_kv_cache *c, const uint16_t *q, int64_t q_stride, const int32_t *cu_q, int32_t n,
                       int32_t total_q, int32_t max_q, const int32_t *blocks, int32_t block_rows, int32_t blocks_stride,

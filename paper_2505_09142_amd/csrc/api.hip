@@ -743,7 +743,7 @@ int check_kv_attention_sizes(int32_t n, int32_t total_q, int32_t max_q, int32_t 
                              int32_t d_head) {
     if (n < 1 || total_q < 0 || max_q < 1 || max_kv < 0 || n_heads < 1 || n_kv_heads < 1 || d_head < 1) return ELIS_EINVAL;
     if (n_heads % n_kv_heads || n_kv_heads > 1024 || n_heads > 16384 || (d_head != 64 && d_head != 128)) return ELIS_EUNSUPPORTED;
-    if (n > 65535) return ELIS_ESHAPE;
+    if (n > 65535 || max_kv > (1 << 30)) return ELIS_ESHAPE;
     // row numbers and launch sizes stay below 2^31
     if (static_cast<int64_t>(max_q) * (n_heads / n_kv_heads) > INT32_MAX / 128 ||
         static_cast<int64_t>(total_q) * n_heads > INT32_MAX / 64)

@@ -187,7 +187,7 @@ hipError_t launch_kv_read(KvCacheView c, const int32_t* map, int n, uint16_t* k,
 struct KvAttnPlan {
     int small, small_nb, small_rows, small_chunk, small_chunks;
     bool many;
-    int many_chunk, many_chunks;
+    int many_tiles, many_chunk, many_chunks;
     size_t small_parts, many_parts;  // chunk results to join (d_head floats and two more each)
 };
 KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads);

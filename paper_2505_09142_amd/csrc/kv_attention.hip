@@ -12,13 +12,15 @@
 // scale), of the values D/16 columns of four keys. E2M1 times a power of two is exact in bf16: one
 // v_cvt_scalef32_pk_bf16_fp4 makes two operands' worth, for V^T followed by one byte permutation that pairs two keys.
 //
-// Softmax: running maximum and sum in fp32; the maximum lags (the accumulators are rescaled only when a score exceeds
-// it by 2^8), the row sum comes from the matrix cores over the bf16 weights that multiply V.
+// Softmax: running maximum and sum in fp32; the maximum lags: the accumulators are rescaled only when a score exceeds it
+// by 2^8, which each lane can tell from its own scores, so the lanes of a row exchange theirs only then. It is kept as a
+// whole number of powers of two, so that rescaling is exact, that of weights in bf16 too. The weights are
+// rounded to bf16 for the second product (half a step, 2^-8 of each); their sum is not.
 //
 // Masks. A key is seen when it is at or before the token's position, inside its window, and on a valid page. Records
 // wholly seen by every row skip the test. The codes of keys that no row may see (past the end, on a bad page) are
 // zeroed, so what lies there cannot matter; a group of values that holds NaN (scale 255) is multiplied as zero and
-// makes NaN of exactly the rows that see it.
+// makes NaN of exactly the rows that see it (where every row sees a record, its NaN goes through the products).
 //
 // Bound by memory for single tokens: 17/16 D bytes a key and kv head, once. The vector unit comes second: about 180
 // instructions a 32-key step of a wave. Few rows are split over the keys (chunks) and joined by a second launch.
@@ -30,15 +32,33 @@ namespace elis {
 
 namespace {
 
+constexpr int kStep = 32;  // keys a wave takes at a time: two records
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kStep = 32;  // keys a wave takes at a time: two records
+constexpr float kLowest = -3.0e38f;  // a maximum over no keys: finite, so that differences of maxima are numbers
+#ifndef XOCC
+#define XOCC 3
+#endif
+constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
 
+// Maxima as single instructions: fmaxf first quiets each operand's signalling NaN with an instruction of its own.
+__device__ __forceinline__ float max2(float x, float y) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return r;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
+// Maximum over the lanes l, l^16, l^32, l^48, which hold one row's scores.
 __device__ __forceinline__ float quad_max(float v) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    v = max2(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return max2(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 template <int D>
@@ -91,25 +111,99 @@ __device__ __forceinline__ int chunks_of(int lo, int hi, int chunk) {
     return n < 1 ? 1 : n;
 }
 
+// Tile `want` of TILE rows among the requests with more than a.small rows, by all kThreads threads of the work-group (the
+// two results are in LDS); false if there are fewer.
+template <int TILE>
+__device__ __forceinline__ bool find_tile(const KvAttnArgs& a, int want, int* req, int* rt) {
+    __shared__ int tot[kWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
+    int before = 0;
+    for (int base = 0; base < a.n; base += kThreads) {
+        const int i = base + tid;
+        int tiles = 0;
+        if (i < a.n) {
+            const int o0 = a.cu[i], o1 = a.cu[i + 1], ql = o1 - o0;
+            if (o0 < 0 || o1 > a.total_q || o1 < o0) atomicOr(a.c.status, ELIS_DEV_BAD_CU);
+            else if (ql > a.max_q) atomicOr(a.c.status, ELIS_DEV_LONG_SEQ);
+            else if (ql * a.group > a.small) tiles = (ql * a.group + TILE - 1) / TILE;
+        }
+        int incl = tiles;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int v = __shfl_up(incl, o, kWave);
+            if (lane >= o) incl += v;
+        }
+        if (base) __syncthreads();  // tot has been read
+        if (lane == kWave - 1) tot[wid] = incl;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wid) incl += tot[w];
+            all += tot[w];
+        }
+        incl += before;
+        before += all;
+        if (want < incl && want >= incl - tiles) {
+            *req = i;
+            *rt = incl - 1 - want;
+        }
+        if (want < before) {
+            __syncthreads();
+            return true;
+        }
+    }
+    return false;
+}
+
 __device__ __forceinline__ float scale_of(uint32_t dword, int byte) {
     return __uint_as_float(((dword >> (8 * byte)) & 0xFFu) << 23);
 }
 
-// Four waves. MANY: rows of every request with more than `small` rows, in tiles; else the others, one tile each.
+// MANY: rows of every request with more than `small` rows, in tiles; else the others, one tile each.
 template <int D, int NB, bool MANY>
-__global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_kernel(KvAttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using R = Rec<D>;
     typedef typename RecRegs<D>::vec vec;
     constexpr int KS = D / 32;   // k-steps of the first product
     constexpr int DB = D / 16;   // 16-row blocks of O^T; values of a column
-    constexpr int CV = D / 64;   // conversions of a column: pairs of values
-    constexpr int CVN = DB / 2;  // = 4 (D 128), 2 (D 64)
-    static_assert(CVN == 2 * CV, "pairs of a column");
+    constexpr bool QLDS = NB == 4;  // 64 query rows in LDS: their registers are what a second wave on the SIMD needs
     __shared__ __attribute__((aligned(16))) float so[kWaves][16][D + 4];
     __shared__ float sm[kWaves][NB * 16], sl[kWaves][NB * 16];
+    __shared__ __attribute__((aligned(16))) bf16x8 sq[QLDS ? NB * KS * kWave : 1];
 
-    const int chunk_i = blockIdx.x % a.nchunks, rt = blockIdx.x / a.nchunks, h = blockIdx.y, req = blockIdx.z;
+    // Heads fastest, then requests, tiles and chunks: the work-groups of one chunk number, which only long requests
+    // have many of, spread over all XCDs (with chunks fastest 8 of them put every first chunk on one XCD: 48 -> 25 us).
+    unsigned unit = blockIdx.x;
+    const int h = static_cast<int>(unit % a.c.n_kv_heads);
+    unit /= a.c.n_kv_heads;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int g = lane >> 4, c = lane & 15;
+    int req, rt = 0, chunk_i;
+    if constexpr (MANY) {
+        // Tiles are numbered through the requests that have more than `small` rows, last tile (most keys) first.
+        __shared__ int found_req, found_rt;
+        chunk_i = static_cast<int>(unit % a.nchunks);
+        if (!find_tile<NB * 16>(a, static_cast<int>(unit / a.nchunks), &found_req, &found_rt)) return;
+        req = found_req;
+        rt = found_rt;
+    } else {
+        req = static_cast<int>(unit % a.n);
+        chunk_i = static_cast<int>(unit / a.n);
+    }
+
+    // The waves take the chunk's 32-key steps in turn; lane l knows the page of record l of its wave's steps (two each,
+    // 32 steps at most). Without a window the keys do not depend on the lengths, and the pages are fetched along with them.
+    const int64_t row = a.rows ? a.rows[req] : req;
+    const bool row_ok = row >= 0 && row < a.block_rows;
+    auto page_of = [&](int key) {
+        const int bi = key >> a.c.page_shift;
+        return row_ok && bi < a.blocks_stride ? a.blocks[row * a.blocks_stride + bi] : -1;
+    };
+    const int my_rec = ((wid + kWaves * (lane >> 1)) * 2 + (lane & 1)) * kRecTokens;  // its first key, from the chunk's
+    int page = a.window > 0 ? 0 : page_of(chunk_i * a.chunk + my_rec);
+
     const Request rq = request_of(a, req);
     const int rows = rq.ql * a.group;
     if (!rq.ok || rows <= 0 || (MANY ? rows <= a.small : rows > a.small)) return;
@@ -121,219 +215,264 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
     const int nc = chunks_of(lo, hi, a.chunk);
     if (chunk_i >= nc) return;
     const int k0 = lo + chunk_i * a.chunk, k1 = k0 + a.chunk < hi ? k0 + a.chunk : hi;
-
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int g = lane >> 4, c = lane & 15;
     const int back = rq.kv - rq.ql;
+    if (a.window > 0) page = page_of(k0 + my_rec);
+
+    int off_lo, off_hi;  // of record `lane` of the wave's steps in the current span, or -1
+    auto place = [&](int span) {
+        long long off = -1;
+        if (span + my_rec < k1) {
+            if (page >= 0 && page < a.c.n_pages)
+                off = static_cast<long long>(rec_offset(a.c, page, h, ((span + my_rec) & (a.c.page_tokens - 1)) / kRecTokens));
+            else
+                atomicOr(a.c.status, ELIS_DEV_BAD_PAGE);
+        }
+        off_lo = static_cast<int>(off);
+        off_hi = static_cast<int>(off >> 32);
+    };
+    place(k0);
+
+    const uint32_t lk = R::key_at(c, g * (D / 8)), lv = R::val_at(4 * g, c), lks = R::scale_k_at(c, g * (D / 4) / 32),
+                   lvs = R::scale_v_at(4 * g, c * DB / 32);
+    // Record x of the wave as a buffer of its bytes; one that is not there is empty and reads as zeros, so loads need no
+    // condition (under one the compiler cannot tell how many are in flight, and waits for all before each step).
+    auto record = [&](int x) {
+        const int lo32 = __builtin_amdgcn_readlane(off_lo, x & 63);
+        const int hi32 = __builtin_amdgcn_readlane(off_hi, x & 63) | ((63 - x) >> 31);  // -1 past the lanes' records
+        uint8_t* rec = a.c.pages + (static_cast<long long>(hi32 & 0x7FFFFFFF) << 32 | static_cast<uint32_t>(lo32));
+        return __builtin_amdgcn_make_buffer_rsrc(rec, 0, hi32 >= 0 ? R::kBytes : 0, 0x00020000);
+    };
+    // A step's two records in registers; the next step's are fetched while this one's are multiplied, into registers of
+    // their own or (INPLACE: they are needed for 64 rows, whose step is long) into these, keys and values each as soon as
+    // they have been used.
+    constexpr bool INPLACE = NB == 4;
+    struct Step {
+        vec k[2], v[2];
+        uint32_t ks[2], vs[2];
+    };
+    auto load_k = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
+        if constexpr (D == 128) x.k[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lk, 0, 0);
+        else x.k[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lk, 0, 0);
+        x.ks[u] = __builtin_amdgcn_raw_buffer_load_b8(rec, lks, 0, 0);
+    };
+    auto load_v = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
+        if constexpr (D == 128) x.v[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lv, 0, 0);
+        else x.v[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lv, 0, 0);
+        x.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lvs, 0, 0);
+    };
+    auto load = [&](int st, Step& x) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const auto rec = record(2 * st + u);
+            load_k(rec, x, u);
+            load_v(rec, x, u);
+        }
+    };
+    Step x;
+    load(0, x);
 
     // Query operands: lane (c, g) holds the D/4 values of row c that lane group g's key bytes cover.
-    bf16x8 qf[NB][KS];
-    int pos[NB], from[NB];
+    bf16x8 qf[QLDS ? 1 : NB][KS];
+    auto token = [&](int j) {  // of row c of block j
+        const int r = r0 + 16 * j + c;
+        return (r < rows ? r : rows - 1) / a.group;
+    };
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         int r = r0 + 16 * j + c;
         r = r < rows ? r : rows - 1;
-        const int t = r / a.group, head = h * a.group + (r - t * a.group);
-        pos[j] = back + t;
-        from[j] = a.window > 0 ? pos[j] - a.window + 1 : 0;
+        const int t = token(j), head = h * a.group + (r - t * a.group);
         const uint16_t* p = a.q + static_cast<long long>(rq.q0 + t) * a.q_stride + static_cast<long long>(head) * D + g * (D / 4);
+        if (QLDS && j != wid) continue;  // wave j fetches block j for all
+        const int jq = QLDS ? 0 : j;
         if (a.q_vec) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[j][s] = *reinterpret_cast<const bf16x8*>(p + 8 * s);
+            for (int s = 0; s < KS; ++s) qf[jq][s] = *reinterpret_cast<const bf16x8*>(p + 8 * s);
         } else {
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = p[8 * s + 2 * e] | (static_cast<uint32_t>(p[8 * s + 2 * e + 1]) << 16);
-                qf[j][s] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+                qf[jq][s] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
             }
         }
     }
+    if constexpr (QLDS) {
+        static_assert(NB == kWaves, "a block of rows a wave");
+#pragma unroll
+        for (int s = 0; s < KS; ++s) sq[(wid * KS + s) * kWave + lane] = qf[0][s];
+        __syncthreads();
+    }
+    auto query = [&](int j, int s) { return QLDS ? sq[(j * KS + s) * kWave + lane] : qf[QLDS ? 0 : j][s]; };
     // Keys that every row sees: [all_lo, all_hi).
     const int all_hi = back + r0 / a.group + 1, all_lo = a.window > 0 ? back + (r1 - 1) / a.group - a.window + 1 : 0;
 
-    // This wave's keys [w0, w1) and the places of its records, one a lane (at most 64: a chunk has at most 4096 keys).
-    const int per = ((k1 - k0 + kWaves - 1) / kWaves + kStep - 1) / kStep * kStep;
-    const int w0 = k0 + wid * per, w1 = w0 + per < k1 ? w0 + per : k1;
-    const int steps = w1 > w0 ? (w1 - w0 + kStep - 1) / kStep : 0;
-    long long my_off = -1;
-    {
-        const int key = w0 + lane * kRecTokens;
-        if (key < w1) {
-            const int bi = key >> a.c.page_shift;
-            const int64_t row = a.rows ? a.rows[req] : req;
-            const int page = row >= 0 && row < a.block_rows ? a.blocks[row * a.blocks_stride + bi] : -1;
-            if (page >= 0 && page < a.c.n_pages)
-                my_off = static_cast<long long>(rec_offset(a.c, page, h, (key & (a.c.page_tokens - 1)) / kRecTokens));
-            else
-                atomicOr(a.c.status, ELIS_DEV_BAD_PAGE);
-        }
-    }
-    const int off_lo = static_cast<int>(my_off), off_hi = static_cast<int>(my_off >> 32);
-
-    struct Load {
-        vec k, v;
-        uint32_t ks, vs;
-    };
-    const uint32_t lk = R::key_at(c, g * (D / 8)), lv = R::val_at(4 * g, c), lks = R::scale_k_at(c, g * (D / 4) / 32),
-                   lvs = R::scale_v_at(4 * g, c * DB / 32);
-    // Record x of the wave: its bytes, and whether it is there.
-    auto load = [&](int x, Load& l) {
-        const int lo32 = __builtin_amdgcn_readlane(off_lo, x & 63), hi32 = __builtin_amdgcn_readlane(off_hi, x & 63);
-        const bool there = hi32 >= 0;
-        const uint8_t* rec = a.c.pages + (there ? (static_cast<long long>(hi32) << 32 | static_cast<uint32_t>(lo32)) : 0);
-        l.k = *reinterpret_cast<const vec*>(rec + lk);
-        l.v = *reinterpret_cast<const vec*>(rec + lv);
-        l.ks = rec[lks];
-        l.vs = *reinterpret_cast<const uint32_t*>(rec + lvs);
-        return there;
-    };
-
-    f32x4 o[DB][NB], lsum[NB];
-    float m[NB];
+    f32x4 o[DB][NB];
+    float m[NB], lsum[NB];  // m in units of log2, a whole number: rescaling is exact; lsum over the lane's own keys
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        m[j] = -INFINITY;
-        lsum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m[j] = kLowest;
+        lsum[j] = 0.f;
 #pragma unroll
         for (int b = 0; b < DB; ++b) o[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    bf16x8 ones;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(1.0f);
-    const float sc = a.scale_log2, lag = 8.0f / sc;
+    const float sc = a.scale_log2;
+    constexpr int UB = INPLACE ? 1 : 2;  // records whose scores are held at a time
 
-    Load nx[2];
-    bool nt[2] = {false, false};
-    if (steps > 0) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) nt[u] = load(u, nx[u]);
-    }
-    for (int st = 0; st < steps; ++st) {
-        Load cur[2] = {nx[0], nx[1]};
-        const bool there[2] = {nt[0], nt[1]};
-        if (st + 1 < steps) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) nt[u] = load(2 * st + 2 + u, nx[u]);
+    for (int span = k0; span < k1; span += kSpan) {  // one where rows are few: such chunks fit
+        if (MANY && span > k0) {
+            page = page_of(span + my_rec);
+            place(span);
+            load(0, x);
         }
-        const int kb = w0 + st * kStep;
-        f32x4 s[2][NB];
+        const int w0 = span + wid * kStep, w1 = span + kSpan < k1 ? span + kSpan : k1;
+        const int steps = w0 < w1 ? (w1 - w0 + kWaves * kStep - 1) / (kWaves * kStep) : 0;
+    for (int st = 0; st < steps; ++st) {
+        // keeps the query rows in LDS: reads of memory that does not change would be moved out of the loop, into registers
+        if constexpr (QLDS) asm volatile("" ::: "memory");
+        Step next;
+        if constexpr (!INPLACE) load(st + 1, next);
+        const int kb = w0 + st * (kWaves * kStep);
+        bool there[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float ksc = __uint_as_float(cur[u].ks << 23);
+        for (int u = 0; u < 2; ++u) there[u] = __builtin_amdgcn_readlane(off_hi, (2 * st + u) & 63) >= 0;
+        // Uniform: some key of the step is not seen by some row.
+        const bool edge = kb + kStep > all_hi || kb < all_lo || !there[0] || !there[1];
+        uint32_t pw[NB][4];  // the weights, as the second product's operand
 #pragma unroll
-            for (int j = 0; j < NB; ++j) s[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int u0 = 0; u0 < 2; u0 += UB) {
+            f32x4 s[UB][NB];
+#pragma unroll
+            for (int u = 0; u < UB; ++u)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) s[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < KS; ++t) {
-                const uint32_t w = cur[u].k[t];
-                const u32x4 kk = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 0)),
-                                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 1)),
-                                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 2)),
-                                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 3))};
+                bf16x8 q[NB];
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
-                    s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), qf[j][t], s[u][j], 0, 0, 0);
-            }
-        }
-        // Uniform: some key of the step is not seen by some row, or holds NaN values.
-        bool nan_v = false;
+                for (int j = 0; j < NB; ++j) q[j] = query(j, t);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint32_t x = ~cur[u].vs;  // a zero byte is a scale of 255
-            nan_v = nan_v || ((x - 0x01010101u) & ~x & 0x80808080u) != 0u;
-        }
-        if (kb + kStep > all_hi || kb < all_lo || !there[0] || !there[1] || __ballot(nan_v) != 0ull) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint32_t poison = 0u;  // rows whose values of this lane's columns become NaN
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = kb + 16 * u + 4 * g + i;
+                for (int u = 0; u < UB; ++u) {
+                    const uint32_t w = x.k[u0 + u][t];
+                    const float ksc = __uint_as_float(x.ks[u0 + u] << 23);
+                    const u32x4 kk = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 0)),
+                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 1)),
+                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 2)),
+                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 3))};
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
-                        if (!there[u] || key > pos[j] || key < from[j]) s[u][j][i] = -INFINITY;
-                    // values that no row may see, or that are NaN, multiply as zero
-                    if (!there[u] || key >= hi || ((cur[u].vs >> (8 * i)) & 0xFFu) == 0xFFu) {
-                        if constexpr (D == 128) cur[u].v[i] = 0u;
-                        else cur[u].v[i >> 1] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;
-                    }
+                        s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), q[j], s[u][j], 0, 0, 0);
                 }
-                if (there[u]) {
-                    // lane (c, g) of O^T holds columns 4g..4g+3: values D/4 g ..., of scale group g D/128
-                    const int grp = g * (D / 4) / 32;
+            }
+            if (edge) {
+                int pos[NB], from[NB];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const uint32_t w = __shfl(cur[u].vs, (x >> 2) * 16 + grp * (32 / DB), kWave);
-                        const int key = kb + 16 * u + x;
-                        if (((w >> (8 * (x & 3))) & 0xFFu) == 0xFFu) {
+                for (int j = 0; j < NB; ++j) {
+                    pos[j] = back + token(j);
+                    from[j] = a.window > 0 ? pos[j] - a.window + 1 : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < UB; ++u) {
+                    const int v = u0 + u, kv = kb + 16 * v;
+                    uint32_t nan = 0u;  // of this lane's four keys, those whose values are NaN
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = kv + 4 * g + i;
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+                            if (!there[v] || key > pos[j] || key < from[j]) s[u][j][i] = -INFINITY;
+                        // values that no row may see, or that are NaN, multiply as zero
+                        const bool is_nan = ((x.vs[v] >> (8 * i)) & 0xFFu) == 0xFFu;
+                        if (is_nan) {
+                            x.vs[v] ^= 0xFFu << (8 * i);
+                            nan |= key < hi ? 1u << i : 0u;
+                        }
+                        if (is_nan || key >= hi) {
+                            if constexpr (D == 128) x.v[v][i] = 0u;
+                            else x.v[v][i >> 1] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                        }
+                    }
+                    if (__ballot(nan != 0u) != 0ull) {
+                        // lane (c, g) of O^T holds columns 4g..4g+3: values D/4 g ..., of the scale group that lane
+                        // (from_c, g') read for the keys 4g'..4g'+3
+                        const int from_c = g * (D / 4) / 32 * (32 / DB);
+#pragma unroll 1
+                        for (int y = 0; y < 16; ++y) {
+                            const uint32_t w = __shfl(nan, (y >> 2) * 16 + from_c, kWave);
 #pragma unroll
                             for (int j = 0; j < NB; ++j)
-                                if (key <= pos[j] && key >= from[j]) poison |= 1u << j;
+                                if (((w >> (y & 3)) & 1u) && kv + y <= pos[j] && kv + y >= from[j]) {
+#pragma unroll
+                                    for (int b = 0; b < DB; ++b) o[b][j] = f32x4{NAN, NAN, NAN, NAN};
+                                }
                         }
                     }
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        if (poison & (1u << j)) {
-#pragma unroll
-                            for (int b = 0; b < DB; ++b)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) o[b][j][i] = __uint_as_float(0x7FC00000u);
-                        }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (((cur[u].vs >> (8 * i)) & 0xFFu) == 0xFFu) cur[u].vs &= ~(0xFFu << (8 * i));
             }
+            if constexpr (INPLACE) load_k(record(2 * st + 2 + u0), x, u0);
+            // The lanes of a row agree on m; whether to raise it each can tell from its own scores.
+            float t[NB], over = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                t[j] = max2(max3(s[0][j][0], s[0][j][1], s[0][j][2]), s[0][j][3]);
+                if constexpr (UB == 2) t[j] = max3(t[j], max3(s[1][j][0], s[1][j][1], s[1][j][2]), s[1][j][3]);
+                over = max2(over, fmaf(t[j], sc, -m[j]));
+            }
+            if (__ballot(over > 8.f) != 0ull) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const float mn = max2(m[j], ceilf(quad_max(t[j]) * sc));
+                    const float w = __builtin_amdgcn_exp2f(m[j] - mn);
+                    m[j] = mn;
+                    lsum[j] *= w;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[b][j][i] *= w;
+                    if (u0 > 0) {  // the first record's weights wait for the second product
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            pw[j][e] = pack_bf16x2(__uint_as_float(pw[j][e] << 16) * w, __uint_as_float(pw[j][e] & 0xFFFF0000u) * w);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int u = 0; u < UB; ++u) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][j][i], sc, -m[j]));
+                    lsum[j] += (p[0] + p[1]) + (p[2] + p[3]);
+                    pw[j][2 * (u0 + u)] = pack_bf16x2(p[0], p[1]);
+                    pw[j][2 * (u0 + u) + 1] = pack_bf16x2(p[2], p[3]);
+                }
         }
         bf16x8 pf[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            float t = fmaxf(fmaxf(fmaxf(s[0][j][0], s[0][j][1]), fmaxf(s[0][j][2], s[0][j][3])),
-                            fmaxf(fmaxf(s[1][j][0], s[1][j][1]), fmaxf(s[1][j][2], s[1][j][3])));
-            t = quad_max(t);
-            if (__ballot(t > m[j] + lag) != 0ull) {  // also the first finite maximum: m is -inf
-                const float mn = fmaxf(m[j], t);
-                const float w = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[j] - mn) * sc);
-                m[j] = mn;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) lsum[j][i] *= w;
-#pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[b][j][i] *= w;
-            }
-            const float ms = m[j] == -INFINITY ? 0.f : m[j] * sc;
-            float p[8];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[4 * u + i] = __builtin_amdgcn_exp2f(fmaf(s[u][j][i], sc, -ms));
-            const u32x4 pw = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
-            pf[j] = __builtin_bit_cast(bf16x8, pw);
-            lsum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[j], lsum[j], 0, 0, 0);
-        }
+        for (int j = 0; j < NB; ++j) pf[j] = __builtin_bit_cast(bf16x8, u32x4{pw[j][0], pw[j][1], pw[j][2], pw[j][3]});
         // V^T: for every pair of a column's values, the eight keys' pairs, then even and odd value as operands of two blocks
         float vsc[8];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vsc[4 * u + i] = scale_of(cur[u].vs, i);
+            for (int i = 0; i < 4; ++i) vsc[4 * u + i] = scale_of(x.vs[u], i);
 #define ELIS_VPAIR(SEL)                                                                                                                \
     {                                                                                                                                  \
-        uint32_t x[8];                                                                                                                 \
+        uint32_t y[8];                                                                                                                 \
         _Pragma("unroll") for (int u = 0; u < 2; ++u) _Pragma("unroll") for (int i = 0; i < 4; ++i) {                                  \
             if constexpr (D == 128)                                                                                                    \
-                x[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cur[u].v[i], vsc[4 * u + i], SEL)); \
+                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i], vsc[4 * u + i], SEL)); \
             else if (i & 1)                                                                                                            \
-                x[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cur[u].v[i >> 1], vsc[4 * u + i], 2 + ((SEL) & 1))); \
+                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i >> 1], vsc[4 * u + i], 2 + ((SEL) & 1))); \
             else                                                                                                                       \
-                x[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(cur[u].v[i >> 1], vsc[4 * u + i], (SEL) & 1)); \
+                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i >> 1], vsc[4 * u + i], (SEL) & 1)); \
         }                                                                                                                              \
         u32x4 ev, od;                                                                                                                  \
         _Pragma("unroll") for (int e = 0; e < 4; ++e) {                                                                                \
-            ev[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x05040100u);                                                        \
-            od[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], 0x07060302u);                                                        \
+            ev[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x05040100u);                                                        \
+            od[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x07060302u);                                                        \
         }                                                                                                                              \
         _Pragma("unroll") for (int j = 0; j < NB; ++j) {                                                                               \
             o[2 * (SEL)][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ev), pf[j], o[2 * (SEL)][j], 0, 0, 0); \
@@ -347,25 +486,35 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
             ELIS_VPAIR(3)
         }
 #undef ELIS_VPAIR
+        if constexpr (INPLACE) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) load_v(record(2 * st + 2 + u), x, u);
+        } else {
+            x = next;
+        }
+    }
     }
 
     // The four waves' parts, joined in wave order.
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
+    for (int j = 0; j < NB; ++j) {
+        lsum[j] += __shfl_xor(lsum[j], 16, kWave);
+        lsum[j] += __shfl_xor(lsum[j], 32, kWave);
         if (g == 0) {
             sm[wid][16 * j + c] = m[j];
-            sl[wid][16 * j + c] = lsum[j][0];
+            sl[wid][16 * j + c] = lsum[j];
         }
+    }
     __syncthreads();
     constexpr int PT = D / 16;  // values a thread joins: 16 threads a row
     const int jr = tid >> 4, jd = (tid & 15) * PT;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         if (16 * j >= r1 - r0) break;  // uniform
-        float top = -INFINITY;
+        float top = kLowest;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w][16 * j + c]);
-        const float wt = m[j] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[j] - top) * sc);
+        const float wt = __builtin_amdgcn_exp2f(m[j] - top);
         if (j) __syncthreads();  // the last block has been read
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -377,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
         __syncthreads();
         const int r = r0 + 16 * j + jr;
         if (r < r1) {
-            float mt = -INFINITY, lt = 0.f;
+            float mt = kLowest, lt = 0.f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) mt = fmaxf(mt, sm[w][16 * j + jr]);
             float acc[PT];
@@ -385,8 +534,7 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
             for (int e = 0; e < PT; ++e) acc[e] = 0.f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float mw = sm[w][16 * j + jr];
-                lt += sl[w][16 * j + jr] * (mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mw - mt) * sc));
+                lt += sl[w][16 * j + jr] * __builtin_amdgcn_exp2f(sm[w][16 * j + jr] - mt);
 #pragma unroll
                 for (int e = 0; e < PT; ++e) acc[e] += so[w][jr][jd + e];
             }
@@ -416,11 +564,14 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(KvAttnArgs a) {
 #endif
 }
 
-// Joins the chunks of split rows, in chunk order: one wave a row.
-template <int D, bool MANY>
+// Joins the chunks of split rows, in an order that depends on their number alone. WAVES waves a row, each taking every
+// WAVES-th chunk: with one wave a row of 118 chunks took 38 us, its loads one behind the other.
+template <int D, bool MANY, int WAVES>
 __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int rows_per, int tile) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const long long w = static_cast<long long>(blockIdx.x) * kWaves + threadIdx.x / kWave;
+    __shared__ __attribute__((aligned(16))) float part[WAVES > 1 ? kWaves : 1][D];
+    const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
+    const long long w = static_cast<long long>(blockIdx.x) * (kWaves / WAVES) + wid / WAVES;
+    const int wi = wid % WAVES;
     int req, h, r;
     if constexpr (MANY) {
         const long long tok = w / a.n_heads;
@@ -443,31 +594,50 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int 
     int lo, hi;
     span_of(a, rq, r0, r1, &lo, &hi);
     const int nc = chunks_of(lo, hi, a.chunk);
-    if (nc == 1) return;
+    if (nc == 1) return;  // every return is the same for the waves of a row
     const int t = r / a.group, head = h * a.group + (r - t * a.group);
     const size_t at = part_row(a, MANY, req, h, rq.q0 + t, head, r) * a.nchunks;
     constexpr int PL = D / kWave;  // values a lane
-    const float sc = a.scale_log2;
-    float top = -INFINITY, total = 0.f, acc[PL];
-#pragma unroll
-    for (int e = 0; e < PL; ++e) acc[e] = 0.f;
+    constexpr int AHEAD = 8;       // chunks a wave fetches at a time, the first before their weights are known
+    typedef float fvec __attribute__((ext_vector_type(PL)));
+    float top = kLowest, total = 0.f;
+    fvec acc = 0.f;
     for (int base = 0; base < nc; base += kWave) {
-        const float2 ml = base + lane < nc ? a.part_ml[at + base + lane] : float2{-INFINITY, 0.f};
-        const float mt = fmaxf(top, wave_max(ml.x));
-        const float old = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((top - mt) * sc);
-        const float wt = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml.x - mt) * sc);
-        total = total * old + wave_sum(ml.y * wt);
-        top = mt;
-#pragma unroll
-        for (int e = 0; e < PL; ++e) acc[e] *= old;
         const int n = nc - base < kWave ? nc - base : kWave;
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float wi = __shfl(wt, i, kWave);
-            const float* p = a.part_o + (at + base + i) * D + lane * PL;
+        const float2 ml = lane < n ? a.part_ml[at + base + lane] : float2{kLowest, 0.f};
+        const float* p = a.part_o + (at + base) * D + lane * PL;
+        fvec v[AHEAD];
+        auto fetch = [&](int i0) {
 #pragma unroll
-            for (int e = 0; e < PL; ++e) acc[e] = fmaf(p[e], wi, acc[e]);
+            for (int y = 0; y < AHEAD; ++y) {
+                const int i = i0 + y * WAVES;
+                v[y] = *reinterpret_cast<const fvec*>(p + (i < n ? i : n - 1) * D);
+            }
+        };
+        fetch(wi);
+        const float mt = fmaxf(top, wave_max(ml.x));
+        const float old = __builtin_amdgcn_exp2f(top - mt), wt = __builtin_amdgcn_exp2f(ml.x - mt);
+        total = total * old + wave_sum(ml.y * wt);
+        acc *= old;
+        top = mt;
+        for (int i0 = wi; i0 < n; i0 += AHEAD * WAVES) {
+            if (i0 > wi) fetch(i0);
+#pragma unroll
+            for (int y = 0; y < AHEAD; ++y) {
+                const int i = i0 + y * WAVES;
+                if (i < n) acc += v[y] * __shfl(wt, i, kWave);  // uniform
+            }
         }
+    }
+    if constexpr (WAVES > 1) {
+#pragma unroll
+        for (int e = 0; e < PL; ++e) part[wid][lane * PL + e] = acc[e];
+        __syncthreads();
+        if (wi != 0) return;
+#pragma unroll
+        for (int x = 1; x < WAVES; ++x)
+#pragma unroll
+            for (int e = 0; e < PL; ++e) acc[e] += part[wid + x][lane * PL + e];
     }
     const float inv = total == 0.f ? 1.0f : 1.0f / total;
     uint16_t* p = a.out + static_cast<long long>(rq.q0 + t) * a.out_stride + static_cast<long long>(head) * D + lane * PL;
@@ -475,41 +645,60 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int 
     for (int e = 0; e < PL; ++e) p[e] = f32_to_bf16(acc[e] * inv);
 }
 
+template <int D, bool MANY>
+hipError_t combine(const KvAttnArgs& a, long long rows, int rows_per, int tile, hipStream_t st) {
+    if (a.nchunks > 8)
+        return launch_kernel(kv_combine_kernel<D, MANY, kWaves>, dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, st, a, rows_per, tile);
+    return launch_kernel(kv_combine_kernel<D, MANY, 1>, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, rows_per, tile);
+}
+
 template <int D>
 hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
     KvAttnArgs a = args;
+    const unsigned per = static_cast<unsigned>(a.c.n_kv_heads) * a.n;
     if (p.small_rows > 0) {
         a.nchunks = p.small_chunks;
         a.chunk = p.small_chunk;
-        const dim3 grid(static_cast<unsigned>(p.small_chunks), static_cast<unsigned>(a.c.n_kv_heads), static_cast<unsigned>(a.n));
         const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : p.small_nb == 2 ? kv_attention_kernel<D, 2, false> : kv_attention_kernel<D, 4, false>;
-        ELIS_TRY(launch_kernel(f, grid, dim3(kThreads), 0, st, a));
-        if (p.small_chunks > 1) {
-            const long long waves = static_cast<long long>(a.n) * a.c.n_kv_heads * p.small_rows;
-            ELIS_TRY(launch_kernel(kv_combine_kernel<D, false>, dim3(static_cast<unsigned>((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a,
-                                   p.small_rows, 16 * p.small_nb));
-        }
+        ELIS_TRY(launch_kernel(f, dim3(per * p.small_chunks), dim3(kThreads), 0, st, a));
+        if (p.small_chunks > 1)
+            ELIS_TRY((combine<D, false>(a, static_cast<long long>(per) * p.small_rows, p.small_rows, 16 * p.small_nb, st)));
     }
-    if (p.many) {
-        const long long tiles = (static_cast<long long>(a.max_q) * a.group + 63) / 64;
-        a.chunk = p.many_chunk;
+    if (p.many_tiles > 0) {
         a.nchunks = p.many_chunks;
-        const dim3 grid(static_cast<unsigned>(tiles * a.nchunks), static_cast<unsigned>(a.c.n_kv_heads), static_cast<unsigned>(a.n));
-        ELIS_TRY(launch_kernel(kv_attention_kernel<D, 4, true>, grid, dim3(kThreads), 0, st, a));
-        if (a.nchunks > 1) {
-            const long long waves = static_cast<long long>(a.total_q) * a.n_heads;
-            ELIS_TRY(launch_kernel(kv_combine_kernel<D, true>, dim3(static_cast<unsigned>((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, 0, 64));
-        }
+        a.chunk = p.many_chunk;
+        ELIS_TRY(launch_kernel(kv_attention_kernel<D, 4, true>, dim3(static_cast<unsigned>(a.c.n_kv_heads) * p.many_tiles * p.many_chunks), dim3(kThreads), 0, st, a));
+        if (p.many_chunks > 1) ELIS_TRY((combine<D, true>(a, static_cast<long long>(a.total_q) * a.n_heads, 0, 64, st)));
     }
     return hipSuccess;
 }
 
+long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
+
 }  // namespace
 
+// Chunks. A work-group needs about 4.5 us whatever its keys and 0.7 us for each 128, and joining costs 4 us, so up to
+// 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001 tokens and 8
+// kv heads: chunks of 512 / 1,024 / 2,048 keys 16.9 / 15.4 / 19.0 us), and at least three to a request that is as long as
+// max_kv, because the others are shorter (64 requests of up to 3,872 tokens: one chunk 25.3, chunks of 1,024 23.5), but
+// not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 / 206).
 KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads) {
     KvAttnPlan p{};
     const int group = n_heads / n_kv_heads;
     const long long most = static_cast<long long>(max_q) * group;
+    auto split = [&](long long work_groups, int least, int* chunk, int* chunks) {
+        long long c = max_kv;
+        if (max_kv > 1024) {
+            long long want = (256 + work_groups - 1) / work_groups;
+            want = want < least ? least : want;
+            if (want > 1) {
+                c = round_up((max_kv + want - 1) / want, 128);
+                c = c < 256 ? 256 : c > 2048 && least > 1 ? 2048 : c;
+            }
+        }
+        *chunk = static_cast<int>(c < 1 ? 1 : round_up(c, 16));
+        *chunks = max_kv > *chunk ? (max_kv + *chunk - 1) / *chunk : 1;
+    };
     // one tile of 16, 32 or 64 rows holds a request, or (of longer ones) at least a single token
     const long long fit = most <= 64 ? most : group;
     if (fit <= 64) {
@@ -518,19 +707,16 @@ KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_he
         p.small_rows = static_cast<int>(most < p.small ? most : p.small);
         p.many = most > p.small;
         if (p.many && static_cast<long long>(n) * max_q == total_q) p.small_rows = 0;  // every request is long
-        const long long per = static_cast<long long>(n) * n_kv_heads;
-        long long want = (2048 + per - 1) / per;  // chunks so that about 2048 work-groups run
-        long long chunk = (max_kv + want - 1) / want;
-        chunk = (chunk + 127) / 128 * 128;
-        chunk = chunk < 256 ? 256 : chunk > 4096 ? 4096 : chunk;
-        p.small_chunk = static_cast<int>(chunk);
-        p.small_chunks = static_cast<int>((max_kv + chunk - 1) / chunk);
-        if (p.small_chunks < 1) p.small_chunks = 1;
+        split(static_cast<long long>(n) * n_kv_heads, 3, &p.small_chunk, &p.small_chunks);
     } else {
         p.many = true;
     }
-    p.many_chunk = 4096;
-    p.many_chunks = p.many && max_kv > 4096 ? (max_kv + 4095) / 4096 : 1;
+    p.many_chunks = 1;
+    if (p.many) {
+        const long long rows = static_cast<long long>(total_q) * group, longer = rows / (p.small + 1);
+        p.many_tiles = static_cast<int>(rows / 64 + (longer < n ? longer : n));  // at most: every long request's last tile cut
+        split((rows / 64 + 1) * n_kv_heads, 1, &p.many_chunk, &p.many_chunks);
+    }
     p.small_parts = p.small_rows > 0 && p.small_chunks > 1 ? static_cast<size_t>(n) * n_kv_heads * p.small_rows * p.small_chunks : 0;
     p.many_parts = p.many && p.many_chunks > 1 ? static_cast<size_t>(total_q) * n_heads * p.many_chunks : 0;
     return p;

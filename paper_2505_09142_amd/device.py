@@ -17,8 +17,8 @@ BF16_KEYS = ("word", "pos", "w_qkv", "w_o", "w_1", "w_2")
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # the handle itself: making torch's stream object costs as much as a launch (2.8 us)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -188,25 +188,32 @@ class JobTable:
         return E.elis_read_status(self.t.base, _stream(stream))
 
 
-def _arg(t: torch.Tensor, dtype: torch.dtype, where: str, at_least: int = 0) -> int:
-    """Address of a contiguous argument of the given type and of at least so many elements."""
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < at_least:
+def _dev() -> int:
+    """The current device: kernels are launched there, so every argument has to be on it."""
+    return torch._C._cuda_getDevice()
+
+
+def _arg(t: torch.Tensor, dtype: torch.dtype, dev: int, where: str, at_least: int = 0) -> int:
+    """Address of a contiguous argument of the given type, on device `dev`, of at least so many elements."""
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < at_least:
         raise E.ElisError(E.ELIS_EINVAL, where)
     return t.data_ptr()
 
 
-def _opt(t: torch.Tensor | None, dtype: torch.dtype, where: str, at_least: int = 0) -> int | None:
-    return None if t is None else _arg(t, dtype, where, at_least)
+def _opt(t: torch.Tensor | None, dtype: torch.dtype, dev: int, where: str, at_least: int = 0) -> int | None:
+    return None if t is None else _arg(t, dtype, dev, where, at_least)
 
 
-def _heads(x: torch.Tensor, heads: int, d: int, where: str) -> int:
+def _heads(x: torch.Tensor, heads: int, d: int, dev: int, where: str) -> int:
     """Token stride of a [tokens, heads, d] or [tokens, heads * d] bf16 tensor whose rows are contiguous."""
-    rows = x.shape[1:]
-    ok = x.dtype == torch.bfloat16 and rows.numel() == heads * d and x.stride(-1) == 1 and \
-        (len(rows) == 1 or (len(rows) == 2 and rows[1] == d and (rows[0] == 1 or x.stride(1) == d)))
-    if not ok:
+    shape = x.shape
+    if len(shape) == 3:
+        ok = shape[1] == heads and shape[2] == d and (heads == 1 or x.stride(1) == d)
+    else:
+        ok = len(shape) == 2 and shape[1] == heads * d
+    if not ok or x.dtype is not torch.bfloat16 or x.get_device() != dev or x.stride(-1) != 1:
         raise E.ElisError(E.ELIS_EINVAL, where)
-    return x.stride(0) if x.shape[0] > 1 else heads * d
+    return x.stride(0) if shape[0] > 1 else heads * d
 
 
 class PagePool:
@@ -226,7 +233,7 @@ class PagePool:
         for t, s in zip(tensors, sizes, strict=True):
             if tuple(t.shape) != s:
                 raise E.ElisError(E.ELIS_ESHAPE, "PagePool")
-            _arg(t, torch.int32, "PagePool")
+            _arg(t, torch.int32, tensors[0].get_device(), "PagePool")
         self.state, self.free_pages, self.held, self.table = tensors
         self.scratch = torch.empty(4 * max_jobs + 4, dtype=torch.int32, device=self.state.device)
         self.p = E.elis_page_pool(*(t.data_ptr() for t in (*tensors, self.scratch)), n_pages, page_tokens, max_jobs,
@@ -238,19 +245,23 @@ class PagePool:
              out_slot_map: torch.Tensor | None, out_blocks: torch.Tensor | None = None, stream=None):
         """Pages for lens[i] tokens of job slots[i]; the slots of the step's total_new new tokens into out_slot_map
         and, if given, the batch's block table into out_blocks [n, width]."""
-        n, i32, where = slots.numel(), torch.int32, "elis_pages_grow"
+        n, i32, dev, where = slots.numel(), torch.int32, self.state.get_device(), "elis_pages_grow"
+        if dev != _dev():
+            raise E.ElisError(E.ELIS_EINVAL, where)
         if out_blocks is not None and (out_blocks.dim() != 2 or out_blocks.shape[0] != n):
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        E.check(E.elis_pages_grow(self.p, _arg(slots, i32, where), _arg(lens, i32, where, n),
-                                  _opt(cu_new, i32, where, n + 1), n, total_new,
-                                  0 if out_blocks is None else out_blocks.shape[1], _opt(out_blocks, i32, where),
-                                  _opt(out_slot_map, i32, where, total_new), _stream(stream)), where)
+        E.check(E.elis_pages_grow(self.p, _arg(slots, i32, dev, where), _arg(lens, i32, dev, where, n),
+                                  _opt(cu_new, i32, dev, where, n + 1), n, total_new,
+                                  0 if out_blocks is None else out_blocks.shape[1], _opt(out_blocks, i32, dev, where),
+                                  _opt(out_slot_map, i32, dev, where, total_new), _stream(stream)), where)
 
     def trim(self, slots: torch.Tensor, lens: torch.Tensor, stream=None):
         """Job slots[i] keeps the pages of its first lens[i] tokens; the others are free again."""
-        where = "elis_pages_trim"
-        E.check(E.elis_pages_trim(self.p, _arg(slots, torch.int32, where),
-                                  _arg(lens, torch.int32, where, slots.numel()), slots.numel(), _stream(stream)), where)
+        n, dev, where = slots.numel(), self.state.get_device(), "elis_pages_trim"
+        if dev != _dev():
+            raise E.ElisError(E.ELIS_EINVAL, where)
+        E.check(E.elis_pages_trim(self.p, _arg(slots, torch.int32, dev, where), _arg(lens, torch.int32, dev, where, n), n,
+                                  _stream(stream)), where)
 
     def status(self, stream=None):
         return E.elis_read_status(self.p.state, _stream(stream))
@@ -270,29 +281,38 @@ class KVCache:
         if made:
             buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
         base = (buf.data_ptr() + 255) // 256 * 256
-        _arg(buf, torch.uint8, "KVCache", base - buf.data_ptr() + nbytes)
-        self.buf = buf
+        _arg(buf, torch.uint8, buf.get_device(), "KVCache", base - buf.data_ptr() + nbytes)
+        self.buf, self.dev = buf, buf.get_device()
         self.c = E.elis_kv_cache(base, n_pages, page_tokens, n_kv_heads, d_head)
         self.ws = Workspace(buf.device)
+        self._sizes, self._need = None, 0  # of the last attention call: its sizes and their workspace
         if made:
             E.check(E.elis_kv_init(self.c, _stream(stream)), "elis_kv_init")
+
+    def _here(self, where: str) -> int:
+        if self.dev != _dev():
+            raise E.ElisError(E.ELIS_EINVAL, where)
+        return self.dev
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream=None):
         """bf16 [tokens, n_kv_heads, d_head] (rows of a wider matrix are taken as they are) into their slots."""
         n, where = slot_map.numel(), "elis_kv_append"
-        ks, vs = (_heads(x, self.n_kv_heads, self.d_head, where) for x in (k, v))
+        dev = self._here(where)
+        ks, vs = _heads(k, self.n_kv_heads, self.d_head, dev, where), _heads(v, self.n_kv_heads, self.d_head, dev, where)
         if k.shape[0] != n or v.shape[0] != n:
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        E.check(E.elis_kv_append(self.c, k.data_ptr(), v.data_ptr(), ks, vs, _arg(slot_map, torch.int32, where), n,
+        E.check(E.elis_kv_append(self.c, k.data_ptr(), v.data_ptr(), ks, vs, _arg(slot_map, torch.int32, dev, where), n,
                                  _stream(stream)), where)
 
     def read(self, slot_map: torch.Tensor, out_k: torch.Tensor, out_v: torch.Tensor, stream=None):
         """What the cache keeps of the tokens in slot_map, as bf16."""
         n, where = slot_map.numel(), "elis_kv_read"
-        ks, vs = (_heads(x, self.n_kv_heads, self.d_head, where) for x in (out_k, out_v))
+        dev = self._here(where)
+        ks = _heads(out_k, self.n_kv_heads, self.d_head, dev, where)
+        vs = _heads(out_v, self.n_kv_heads, self.d_head, dev, where)
         if out_k.shape[0] != n or out_v.shape[0] != n:
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        E.check(E.elis_kv_read(self.c, _arg(slot_map, torch.int32, where), n, out_k.data_ptr(), out_v.data_ptr(), ks, vs,
+        E.check(E.elis_kv_read(self.c, _arg(slot_map, torch.int32, dev, where), n, out_k.data_ptr(), out_v.data_ptr(), ks, vs,
                                _stream(stream)), where)
 
     def attention(self, q: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, blocks: torch.Tensor, max_q: int,
@@ -300,21 +320,24 @@ class KVCache:
                   out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Causal attention of the new tokens q (bf16 [tokens, n_heads, d_head]) over the cache. ``blocks`` holds a
         row of page ids for every request, or, with ``rows``, for every job slot (a pool's table)."""
-        n, where = kv_lens.numel(), "elis_kv_attention"
+        n, i32, where = kv_lens.numel(), torch.int32, "elis_kv_attention"
+        dev = self._here(where)
         if q.dim() != 3 or blocks.dim() != 2 or q.shape[2] != self.d_head:
             raise E.ElisError(E.ELIS_ESHAPE, where)
         total, heads = q.shape[0], q.shape[1]
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        qs, os_ = (_heads(x, heads, self.d_head, where) for x in (q, out))
+        qs, os_ = _heads(q, heads, self.d_head, dev, where), _heads(out, heads, self.d_head, dev, where)
         if out.shape[0] != total:
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        i32 = torch.int32
-        need = E.elis_kv_attention_workspace_bytes(n, total, max_q, max_kv, heads, self.n_kv_heads, self.d_head)
-        ws, wsb = self.ws.get(need)
-        E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, where, n + 1), n, total, max_q,
-                                    _arg(blocks, i32, where), blocks.shape[0], blocks.shape[1],
-                                    _opt(rows, i32, where, n), _arg(kv_lens, i32, where), max_kv, heads,
+        sizes = (n, total, max_q, max_kv, heads)
+        if sizes != self._sizes:
+            self._need = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, self.d_head)
+            self._sizes = sizes
+        ws, wsb = self.ws.get(self._need)
+        E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, dev, where, n + 1), n, total, max_q,
+                                    _arg(blocks, i32, dev, where), blocks.shape[0], blocks.shape[1],
+                                    _opt(rows, i32, dev, where, n), _arg(kv_lens, i32, dev, where), max_kv, heads,
                                     self.d_head ** -0.5 if scale is None else scale, window, out.data_ptr(), os_, ws, wsb,
                                     _stream(stream)), where)
         return out
@@ -328,26 +351,31 @@ def adjust_logits(logits: torch.Tensor, token_ids: torch.Tensor | None, cu_seqle
                   bias=None, mask=None, mask_rows=None, stream=None) -> torch.Tensor:
     """elis_logits_adjust on [n, vocab] logits (bf16 or fp32, rows contiguous). token_ids / cu_seqlens: the histories
     as JobTable.pack writes them. bias: (cu [n + 1], tokens, values). mask: int32 or uint32 [n_masks, words]."""
-    where = "elis_logits_adjust"
-    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1:
+    where, dev = "elis_logits_adjust", _dev()
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1 or \
+            logits.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
     n, vocab = logits.shape
     if out is None:
         out = torch.empty((n, vocab), dtype=torch.float32, device=logits.device)
-    if out.shape != logits.shape or out.dtype != torch.float32 or out.stride(1) != 1 or \
-            (mask is not None and (mask.dim() != 2 or mask.dtype not in (torch.int32, torch.uint32))):
+    if out.shape != logits.shape or out.dtype is not torch.float32 or out.stride(1) != 1 or out.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
     f32, i32 = torch.float32, torch.int32
     b_cu, b_tok, b_val = bias if bias is not None else (None, None, None)
     total = 0 if token_ids is None else token_ids.numel()
     n_bias = 0 if b_tok is None else b_tok.numel()
-    row = lambda x: x.stride(0) if n > 1 else vocab  # noqa: E731
-    E.check(E.elis_logits_adjust(logits.data_ptr(), E.ELIS_DT_BF16 if logits.dtype == torch.bfloat16 else E.ELIS_DT_F32,
-                                 row(logits), n, vocab, _opt(token_ids, i32, where), _opt(cu_seqlens, i32, where, n + 1),
-                                 total, _opt(prompt_lens, i32, where, n), _opt(repetition, f32, where, n),
-                                 _opt(frequency, f32, where, n), _opt(presence, f32, where, n),
-                                 _opt(b_cu, i32, where, n + 1), _opt(b_tok, i32, where), _opt(b_val, f32, where, n_bias),
-                                 n_bias, _opt(mask, mask.dtype if mask is not None else i32, where),
-                                 0 if mask is None else mask.shape[0], 0 if mask is None else mask.shape[1],
-                                 _opt(mask_rows, i32, where, n), out.data_ptr(), row(out), _stream(stream)), where)
+    masks = words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.dtype not in (torch.int32, torch.uint32):
+            raise E.ElisError(E.ELIS_EINVAL, where)
+        masks, words = mask.shape
+    E.check(E.elis_logits_adjust(logits.data_ptr(), E.ELIS_DT_F32 if logits.dtype is f32 else E.ELIS_DT_BF16,
+                                 logits.stride(0) if n > 1 else vocab, n, vocab, _opt(token_ids, i32, dev, where),
+                                 _opt(cu_seqlens, i32, dev, where, n + 1), total, _opt(prompt_lens, i32, dev, where, n),
+                                 _opt(repetition, f32, dev, where, n), _opt(frequency, f32, dev, where, n),
+                                 _opt(presence, f32, dev, where, n), _opt(b_cu, i32, dev, where, n + 1),
+                                 _opt(b_tok, i32, dev, where), _opt(b_val, f32, dev, where, n_bias), n_bias,
+                                 None if mask is None else _arg(mask, mask.dtype, dev, where), masks, words,
+                                 _opt(mask_rows, i32, dev, where, n), out.data_ptr(),
+                                 out.stride(0) if n > 1 else vocab, _stream(stream)), where)
     return out
