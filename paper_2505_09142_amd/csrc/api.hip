@@ -707,7 +707,7 @@ int check_pool(const elis_page_pool* p) {
 }
 
 PagePoolView pool_view(const elis_page_pool* p) {
-    return PagePoolView{p->state, p->free_pages, p->held, p->table, p->scratch,
+    return PagePoolView{p->state, p->free_pages, p->held, p->table, p->scratch, (reinterpret_cast<uintptr_t>(p->scratch) & 15) == 0,
                         p->n_pages, p->page_tokens, log2_of(p->page_tokens), p->max_jobs, p->max_pages};
 }
 

@@ -161,6 +161,7 @@ struct PagePoolView {
     int32_t* held;        // [max_jobs]
     int32_t* table;       // [max_jobs, max_pages]
     int32_t* scratch;     // [4 * max_jobs + 4]
+    bool scratch_vec;     // 16-byte aligned
     int n_pages, page_tokens, page_shift, max_jobs, max_pages;
 };
 hipError_t launch_pages_init(PagePoolView p, hipStream_t st);

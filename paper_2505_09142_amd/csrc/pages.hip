@@ -7,11 +7,11 @@
 // call: the selection's priority order). The slot of the token at position p is table[p / P] * P + p % P. trim takes the
 // pages past a shorter length back, in the order that makes it the exact inverse of grow.
 //
-// Both are a scan over the batch (one work-group, pages_scan_kernel) and then independent work for every job
-// (pages_fill): its new table entries, its row of the batch's block table, and a slot for each new token. Small
-// batches do both in the one work-group's launch; larger ones hand each job's part to a work-group (or several) of a
-// second launch. What the second part needs of the first is left in the pool's scratch: for each entry of the call
-// the stack place of its first page that moves, and its pages before the call.
+// Both are a scan over the batch by one work-group and then independent work for every job: its new table entries, its
+// row of the batch's block table, and a slot for each new token. Small batches do both in one launch (pages_small_kernel:
+// the entries in LDS, the work spread over all threads); larger ones leave what the second part needs in the pool's
+// scratch (for each entry of the call the stack place of its first page that moves, and its pages before and after) and
+// hand each job's part to a work-group (or several) of a second launch. Bound by latency: a few dependent loads.
 #include "kernels.h"
 
 namespace elis {
@@ -19,6 +19,9 @@ namespace elis {
 namespace {
 
 constexpr int kScan = 1024;   // threads of the scan
+constexpr int kEach = 2;      // entries a thread of it holds at a time (2,048 entries: 1 / 2 / 4 of them 11.2 / 10.7 / 12.0 us)
+constexpr int kSmall = 128;   // entries up to which one launch does all,
+constexpr int kSmallWork = 32768;  // with at most so many cells and slots to write
 constexpr int kFill = 256;    // threads of a work-group of the second launch
 constexpr int32_t kClaim = INT32_MIN;  // held[s] with its top bit set: named by an entry of the running call
 
@@ -80,92 +83,259 @@ __device__ __forceinline__ void pages_fill(const FillArgs& a, int i, int32_t s, 
     }
 }
 
-template <bool GROW, bool FUSED>
-__global__ __launch_bounds__(kScan) void pages_scan_kernel(FillArgs a) {
+// Pages that entry (len, new tokens [o0, o1)) of a job that holds h0 moves, and the content errors it shows.
+template <bool GROW>
+__device__ __forceinline__ int pages_move(const FillArgs& a, int i, int len, int o0, int o1, int h0, uint32_t* bad) {
+    if (GROW && a.map &&
+        (o0 < 0 || o1 < o0 || o1 > a.total || (i == 0 && o0 != 0) || (i == a.n - 1 && o1 != a.total) || o1 - o0 > len))
+        *bad |= ELIS_DEV_BAD_CU;
+    const long long want = (static_cast<long long>(len) + a.p.page_tokens - 1) >> a.p.page_shift;
+    if (len < 0) {
+        *bad |= ELIS_DEV_BAD_SLOT;
+        return 0;
+    }
+    if (GROW && want > a.p.max_pages) {
+        *bad |= ELIS_DEV_LONG_SEQ;
+        return 0;
+    }
+    return GROW ? (want > h0 ? static_cast<int>(want) - h0 : 0) : (want < h0 ? h0 - static_cast<int>(want) : 0);
+}
+
+// Inclusive sum over the threads of a work-group of kScan, and the total.
+__device__ __forceinline__ int block_scan(int v, int32_t* wave_tot, int* total) {
     constexpr int kW = kScan / kWave;
-    __shared__ int32_t wave_tot[kW];
-    __shared__ int32_t sh_first[FUSED ? kScan : 1], sh_h0[FUSED ? kScan : 1], sh_h1[FUSED ? kScan : 1], sh_slot[FUSED ? kScan : 1];
+    const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int u = __shfl_up(v, o, kWave);
+        if (lane >= o) v += u;
+    }
+    if (lane == kWave - 1) wave_tot[wid] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+        const int u = wave_tot[w];
+        if (w < wid) before += u;
+        all += u;
+    }
+    *total = all;
+    return v + before;
+}
+
+// Up to kSmall entries, everything in one launch.
+template <bool GROW>
+__global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
+    __shared__ int32_t wave_tot[kScan / kWave];
+    __shared__ int32_t slot[kSmall], first[kSmall], h0s[kSmall], h1s[kSmall], lens[kSmall], cu[kSmall + 1], again[kSmall];
     __shared__ int32_t taken_s;
     __shared__ uint32_t bad_s;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
+    const int tid = threadIdx.x, i = tid;
     if (tid == 0) {
         bad_s = 0u;
         taken_s = 0;
     }
     const int count = clamp_count(a.p.state[1], a.p.n_pages);
     uint32_t bad = 0u;
+    int32_t s = -1;
+    int len = 0, h0 = 0, o0 = 0, o1 = 0;
+    if (i < kSmall) {
+        const int ic = i < a.n ? i : a.n - 1;
+        s = a.slots[ic];
+        len = a.lens[ic];
+        if (GROW && a.map) {
+            o0 = a.cu[ic];
+            o1 = a.cu[ic + 1];
+            cu[i] = o0;
+            if (i == a.n - 1) cu[a.n] = o1;
+        }
+        if (i >= a.n) {
+            s = -1;
+        } else if (s < 0 || s >= a.p.max_jobs) {
+            bad |= ELIS_DEV_BAD_SLOT;
+            s = -1;
+        } else {
+            h0 = clamp_held(a.p.held[s], a.p.max_pages);
+        }
+        slot[i] = s;
+        lens[i] = len;
+        h0s[i] = h0;
+        again[i] = 0;
+    }
     __syncthreads();
-    // First pass: claim every slot (a slot named twice keeps its first claim), pages that move per entry, their prefix.
-    int carry = 0, taken = 0;
-    for (int base = 0; base < a.n; base += kScan) {
-        const int i = base + tid;
-        int32_t s = -1;
-        int move = 0, h0 = 0;
-        if (i < a.n) {
-            s = a.slots[i];
-            const int len = a.lens[i];
-            if (s < 0 || s >= a.p.max_jobs) {
-                bad |= ELIS_DEV_BAD_SLOT;
-                s = -1;
-            } else {
-                const int32_t old = atomicOr(&a.p.held[s], kClaim);
-                h0 = clamp_held(old, a.p.max_pages);
-                const long long want = (static_cast<long long>(len) + a.p.page_tokens - 1) >> a.p.page_shift;
-                if (old & kClaim) {
-                    bad |= ELIS_DEV_BAD_SLOT;
-                } else if (len < 0) {
-                    bad |= ELIS_DEV_BAD_SLOT;
-                } else if (GROW && want > a.p.max_pages) {
-                    bad |= ELIS_DEV_LONG_SEQ;
-                } else {
-                    move = GROW ? (want > h0 ? static_cast<int>(want) - h0 : 0) : (want < h0 ? h0 - static_cast<int>(want) : 0);
-                }
-            }
-            if (GROW && a.map) {
-                const int o0 = a.cu[i], o1 = a.cu[i + 1];
-                if (o0 < 0 || o1 < o0 || o1 > a.total || (i == 0 && o0 != 0) || (i == a.n - 1 && o1 != a.total) || o1 - o0 > len)
-                    bad |= ELIS_DEV_BAD_CU;
-            }
+    // A slot that an earlier entry names too: that one is served. Each wave compares eight entries with all (an entry's
+    // thread alone, with all before it, took 1.2 us longer).
+    const int wid = tid / kWave, lane = tid & (kWave - 1);
+    static_assert(kSmall == 2 * kWave && kSmall == 8 * (kScan / kWave), "two entries a lane, eight a wave");
+    {
+        const int s0 = slot[lane], s1 = slot[lane + kWave];
+        bool d0 = false, d1 = false;
+        for (int j = 8 * wid; j < 8 * wid + 8 && j < a.n; ++j) {
+            const int sj = slot[j];
+            d0 |= sj == s0 && j < lane;
+            d1 |= sj == s1 && j < lane + kWave;
         }
-        int incl = move;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int v = __shfl_up(incl, o, kWave);
-            if (lane >= o) incl += v;
-        }
-        if (lane == kWave - 1) wave_tot[wid] = incl;
-        __syncthreads();
-        int before = carry, all = 0;
-#pragma unroll
-        for (int w = 0; w < kW; ++w) {
-            const int v = wave_tot[w];
-            if (w < wid) before += v;
-            all += v;
-        }
-        incl += before;
-        carry += all;
-        const int off = incl - move;
-        int first, h1;
-        if constexpr (GROW) {
+        if (d0) again[lane] = 1;
+        if (d1) again[lane + kWave] = 1;
+    }
+    __syncthreads();
+    int move = 0;
+    if (i < a.n && s >= 0) {
+        if (again[i]) bad |= ELIS_DEV_BAD_SLOT;
+        else move = pages_move<GROW>(a, i, len, o0, o1, h0, &bad);
+    }
+    int total;
+    const int incl = block_scan(move, wave_tot, &total);
+    int h1 = h0;
+    if (i < a.n) {
+        if (GROW) {
             const bool fits = move == 0 || incl <= count;
             if (!fits) bad |= ELIS_DEV_NO_PAGES;
-            h1 = fits ? h0 + move : h0;
-            first = count - 1 - off;
-            if (move > 0 && fits && incl > taken) taken = incl;
+            else h1 = h0 + move;
+            if (move > 0 && fits) atomicMax(&taken_s, incl);
+            first[i] = count - 1 - (incl - move);
         } else {
             h1 = h0 - move;
-            first = count - 1 - off;  // the total is added once it is known
+            first[i] = count + total - 1 - (incl - move);
         }
-        if (i < a.n) {
-            if constexpr (FUSED) {
-                sh_first[i] = first;
-                sh_h0[i] = h0;
-                sh_h1[i] = h1;
-                sh_slot[i] = s;
-            } else {
-                a.p.scratch[4 * static_cast<size_t>(i)] = first;
-                a.p.scratch[4 * static_cast<size_t>(i) + 1] = h0;
-                a.p.scratch[4 * static_cast<size_t>(i) + 2] = h1;
+        h1s[i] = h1;
+        if (h1 != h0) a.p.held[s] = h1;
+    }
+    if (bad) atomicOr(&bad_s, bad);
+    __syncthreads();
+    if (tid == 0) {
+        const int now = GROW ? count - taken_s : count + total;
+        a.p.state[1] = now < a.p.n_pages ? now : a.p.n_pages;
+        if (bad_s) atomicOr(reinterpret_cast<uint32_t*>(&a.p.state[0]), bad_s);
+    }
+    auto page = [&](int k, int j) {  // of entry k, j < h1
+        return j < h0s[k] ? a.p.table[static_cast<size_t>(slot[k]) * a.p.max_pages + j] : a.p.free_pages[first[k] - (j - h0s[k])];
+    };
+    for (int k = wid; k < a.n; k += kScan / kWave) {  // pages that move
+        const int p0 = GROW ? h0s[k] : h1s[k], p1 = GROW ? h1s[k] : h0s[k];
+        int32_t* row = p1 > p0 ? a.p.table + static_cast<size_t>(slot[k]) * a.p.max_pages : nullptr;
+        for (int j = p0 + lane; j < p1; j += kWave) {
+            const int at = first[k] - (j - p0);
+            if (GROW) row[j] = a.p.free_pages[at];
+            else if (at >= 0 && at < a.p.n_pages) a.p.free_pages[at] = row[j];
+        }
+    }
+    if (GROW && a.blocks) {
+        // Cell x is (x / width, x % width). Each load's address is chosen, not the load: eight are in flight at once. (More
+        // of them, or the comparison of slots unrolled, cost more in fetching the code than they save: 7.6 -> 11.8 us.)
+        constexpr int U = 8;
+        const int cells = a.n * a.width, dk = kScan / a.width, dj = kScan - dk * a.width;
+        int k = tid / a.width, j = tid - k * a.width;
+        for (int x = tid; x < cells; x += U * kScan) {
+            int32_t v[U];
+            bool in[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                in[u] = x + u * kScan < cells;
+                const int kc = in[u] ? k : 0, h0k = h0s[kc];
+                const bool has = in[u] && j < h1s[kc];
+                const int32_t* from = a.slots;
+                if (has) from = j < h0k ? a.p.table + static_cast<size_t>(slot[kc]) * a.p.max_pages + j : a.p.free_pages + (first[kc] - (j - h0k));
+                v[u] = *from;
+                v[u] = has ? v[u] : -1;
+                k += dk;
+                j += dj;
+                if (j >= a.width) {
+                    j -= a.width;
+                    ++k;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (in[u]) a.blocks[x + u * kScan] = v[u];
+        }
+    }
+    if (GROW && a.map) {
+        for (int t = tid; t < a.total; t += kScan) {
+            const int k = find_segment(cu, a.n, t);
+            const int c0 = cu[k], c1 = cu[k + 1];
+            if (t < c0 || t >= c1) continue;  // malformed offsets, flagged above
+            const long long pos = static_cast<long long>(lens[k]) - (c1 - c0) + (t - c0);
+            int32_t at = -1;
+            if (pos >= 0) {
+                const long long j = pos >> a.p.page_shift;
+                if (j < h1s[k]) at = (page(k, static_cast<int>(j)) << a.p.page_shift) + static_cast<int>(pos & (a.p.page_tokens - 1));
+            }
+            a.map[t] = at;
+        }
+    }
+}
+
+// Any number of entries: the scan alone.
+template <bool GROW>
+__global__ __launch_bounds__(kScan) void pages_scan_kernel(FillArgs a) {
+    __shared__ int32_t wave_tot[kScan / kWave];
+    __shared__ int32_t taken_s;
+    __shared__ uint32_t bad_s;
+    const int tid = threadIdx.x;
+    if (tid == 0) {
+        bad_s = 0u;
+        taken_s = 0;
+    }
+    const int count = clamp_count(a.p.state[1], a.p.n_pages);
+    uint32_t bad = 0u;
+    // First pass: claim every slot (a slot named twice keeps its first claim), pages that move per entry, their prefix.
+    int carry = 0, taken = 0;
+    for (int base = 0; base < a.n; base += kEach * kScan) {
+        const int i0 = base + kEach * tid;
+        int32_t s[kEach];
+        int len[kEach], o[kEach + 1] = {}, h0[kEach], move[kEach], sum = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e < a.n ? i0 + e : a.n - 1;  // loads without a condition are all in flight at once
+            s[e] = a.slots[i];
+            len[e] = a.lens[i];
+        }
+        if (GROW && a.map) {
+#pragma unroll
+            for (int e = 0; e <= kEach; ++e) o[e] = a.cu[i0 + e < a.n ? i0 + e : a.n];
+        }
+        int32_t old[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const bool ok = i0 + e < a.n && s[e] >= 0 && s[e] < a.p.max_jobs;
+            if (!ok) s[e] = -1;
+            old[e] = ok ? atomicOr(&a.p.held[s[e]], kClaim) : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            move[e] = h0[e] = 0;
+            if (i0 + e < a.n) {
+                if (s[e] < 0 || (old[e] & kClaim)) bad |= ELIS_DEV_BAD_SLOT;
+                if (s[e] >= 0) {
+                    h0[e] = clamp_held(old[e], a.p.max_pages);
+                    if (!(old[e] & kClaim)) move[e] = pages_move<GROW>(a, i0 + e, len[e], o[e], o[e + 1], h0[e], &bad);
+                }
+            }
+            sum += move[e];
+        }
+        int all;
+        int incl = block_scan(sum, wave_tot, &all) + carry - sum;
+        carry += all;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e, first = count - 1 - incl;  // trim: the total is added once it is known
+            incl += move[e];
+            int h1 = GROW ? h0[e] : h0[e] - move[e];
+            if (GROW) {
+                if (move[e] == 0 || incl <= count) h1 += move[e];
+                else bad |= ELIS_DEV_NO_PAGES;
+                if (h1 != h0[e]) taken = incl;
+            }
+            if (i < a.n) {
+                int4* out = reinterpret_cast<int4*>(a.p.scratch + 4 * static_cast<size_t>(i));
+                const int4 v = {first, h0[e], h1, 0};
+                if (a.p.scratch_vec) *out = v;
+                else {
+                    a.p.scratch[4 * static_cast<size_t>(i)] = v.x;
+                    a.p.scratch[4 * static_cast<size_t>(i) + 1] = v.y;
+                    a.p.scratch[4 * static_cast<size_t>(i) + 2] = v.z;
+                }
             }
         }
         __syncthreads();  // wave_tot is free
@@ -173,27 +343,11 @@ __global__ __launch_bounds__(kScan) void pages_scan_kernel(FillArgs a) {
     if (taken) atomicMax(&taken_s, taken);
     if (bad) atomicOr(&bad_s, bad);
     __syncthreads();
-    const int total = carry;  // trim: pages that return
-    // Second pass: the new counts (a claim of the call ends; an entry whose slot was claimed before it wrote h0 = h1).
     if (tid == 0) {
-        const int now = GROW ? count - taken_s : count + total;
+        const int now = GROW ? count - taken_s : count + carry;
         a.p.state[1] = now < a.p.n_pages ? now : a.p.n_pages;
-        if (!FUSED && !GROW) a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)] = total;
+        if (!GROW) a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)] = carry;
         if (bad_s) atomicOr(reinterpret_cast<uint32_t*>(&a.p.state[0]), bad_s);
-    }
-    for (int base = 0; base < a.n; base += kScan) {
-        const int i = base + tid;
-        if (i >= a.n) break;
-        const int32_t s = a.slots[i];
-        if (s < 0 || s >= a.p.max_jobs) continue;
-        const int h0 = FUSED ? sh_h0[i] : a.p.scratch[4 * static_cast<size_t>(i) + 1];
-        const int h1 = FUSED ? sh_h1[i] : a.p.scratch[4 * static_cast<size_t>(i) + 2];
-        if (h1 != h0) a.p.held[s] = h1;
-        else atomicAnd(&a.p.held[s], ~kClaim);
-    }
-    if constexpr (FUSED) {
-        for (int i = wid; i < a.n; i += kW)
-            pages_fill<GROW>(a, i, sh_slot[i], sh_first[i] + (GROW ? 0 : total), sh_h0[i], sh_h1[i], lane, kWave);
     }
 }
 
@@ -201,8 +355,15 @@ template <bool GROW>
 __global__ __launch_bounds__(kFill) void pages_fill_kernel(FillArgs a, int parts) {
     const int i = blockIdx.x / parts, part = blockIdx.x - i * parts;
     const int32_t* e = a.p.scratch + 4 * static_cast<size_t>(i);
-    const int first = e[0] + (GROW ? 0 : a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)]);
-    pages_fill<GROW>(a, i, a.slots[i], first, e[1], e[2], part * kFill + threadIdx.x, parts * kFill);
+    const int first = e[0] + (GROW ? 0 : a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)]), h0 = e[1], h1 = e[2];
+    const int32_t s = a.slots[i];
+    // The claim of the scan ends: with the new count, or, where nothing moves, by itself (an entry whose slot an earlier
+    // one had claimed moves nothing).
+    if (part == 0 && threadIdx.x == 0 && s >= 0 && s < a.p.max_jobs) {
+        if (h1 != h0) a.p.held[s] = h1;
+        else atomicAnd(&a.p.held[s], ~kClaim);
+    }
+    pages_fill<GROW>(a, i, s, first, h0, h1, part * kFill + threadIdx.x, parts * kFill);
 }
 
 __global__ __launch_bounds__(kFill) void pages_init_kernel(PagePoolView p) {
@@ -218,9 +379,8 @@ __global__ __launch_bounds__(kFill) void pages_init_kernel(PagePoolView p) {
 template <bool GROW>
 hipError_t launch_pages(const FillArgs& a, hipStream_t st) {
     const long long work = GROW ? static_cast<long long>(a.map ? a.total : 0) + (a.blocks ? static_cast<long long>(a.n) * a.width : 0) : 0;
-    if (a.n <= 128 && work <= 32768)
-        return launch_kernel(pages_scan_kernel<GROW, true>, dim3(1), dim3(kScan), 0, st, a);
-    ELIS_TRY(launch_kernel(pages_scan_kernel<GROW, false>, dim3(1), dim3(kScan), 0, st, a));
+    if (a.n <= kSmall && work <= kSmallWork) return launch_kernel(pages_small_kernel<GROW>, dim3(1), dim3(kScan), 0, st, a);
+    ELIS_TRY(launch_kernel(pages_scan_kernel<GROW>, dim3(1), dim3(kScan), 0, st, a));
     long long parts = work / (static_cast<long long>(a.n) * 4 * kFill);  // about four elements a thread
     parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
     if (parts * a.n > 65536) parts = 1;
