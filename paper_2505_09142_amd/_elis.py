@@ -264,8 +264,11 @@ def elis_pool_head(w: elis_weights, hidden: int, cu_seqlens: int, n_seqs: int, t
                                 total_tokens, max_seqlen, out_pred, workspace, ws_bytes, stream)
 
 
+_byref = ctypes.byref
+
+
 def _tab(t):
-    return ctypes.byref(t) if t is not None else None
+    return None if t is None else _byref(t)
 
 
 def elis_jobs_table_bytes(max_jobs: int, max_pos: int) -> int:
@@ -316,11 +319,11 @@ def elis_pages_init(p: elis_page_pool, stream: int | None) -> int:
 
 def elis_pages_grow(p: elis_page_pool, slots: int, lens: int, cu_new: int | None, n: int, total_new: int, width: int,
                     out_blocks: int | None, out_slot_map: int | None, stream: int | None) -> int:
-    return lib().elis_pages_grow(_tab(p), slots, lens, cu_new, n, total_new, width, out_blocks, out_slot_map, stream)
+    return (_lib or lib()).elis_pages_grow(_tab(p), slots, lens, cu_new, n, total_new, width, out_blocks, out_slot_map, stream)
 
 
 def elis_pages_trim(p: elis_page_pool, slots: int, lens: int, n: int, stream: int | None) -> int:
-    return lib().elis_pages_trim(_tab(p), slots, lens, n, stream)
+    return (_lib or lib()).elis_pages_trim(_tab(p), slots, lens, n, stream)
 
 
 def elis_kv_cache_bytes(n_pages: int, page_tokens: int, n_kv_heads: int, d_head: int) -> int:
@@ -333,12 +336,12 @@ def elis_kv_init(c: elis_kv_cache, stream: int | None) -> int:
 
 def elis_kv_append(c: elis_kv_cache, k: int, v: int, k_stride: int, v_stride: int, slot_map: int, n_tokens: int,
                    stream: int | None) -> int:
-    return lib().elis_kv_append(_tab(c), k, v, k_stride, v_stride, slot_map, n_tokens, stream)
+    return (_lib or lib()).elis_kv_append(_tab(c), k, v, k_stride, v_stride, slot_map, n_tokens, stream)
 
 
 def elis_kv_read(c: elis_kv_cache, slot_map: int, n_tokens: int, out_k: int, out_v: int, k_stride: int, v_stride: int,
                  stream: int | None) -> int:
-    return lib().elis_kv_read(_tab(c), slot_map, n_tokens, out_k, out_v, k_stride, v_stride, stream)
+    return (_lib or lib()).elis_kv_read(_tab(c), slot_map, n_tokens, out_k, out_v, k_stride, v_stride, stream)
 
 
 def elis_kv_attention_workspace_bytes(n: int, total_q: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int,
@@ -350,7 +353,7 @@ def elis_kv_attention(c: elis_kv_cache, q: int, q_stride: int, cu_q: int, n: int
                       block_rows: int, blocks_stride: int, rows: int | None, kv_lens: int, max_kv: int, n_heads: int,
                       scale: float, window: int, out: int, out_stride: int, workspace: int, ws_bytes: int,
                       stream: int | None) -> int:
-    return lib().elis_kv_attention(_tab(c), q, q_stride, cu_q, n, total_q, max_q, blocks, block_rows, blocks_stride,
+    return (_lib or lib()).elis_kv_attention(_tab(c), q, q_stride, cu_q, n, total_q, max_q, blocks, block_rows, blocks_stride,
                                    rows, kv_lens, max_kv, n_heads, scale, window, out, out_stride, workspace, ws_bytes,
                                    stream)
 
@@ -360,7 +363,7 @@ def elis_logits_adjust(logits: int, dtype: int, in_stride: int, n: int, vocab: i
                        frequency: int | None, presence: int | None, bias_cu: int | None, bias_tokens: int | None,
                        bias_values: int | None, bias_total: int, mask: int | None, n_masks: int, mask_stride: int,
                        mask_rows: int | None, out: int, out_stride: int, stream: int | None) -> int:
-    return lib().elis_logits_adjust(logits, dtype, in_stride, n, vocab, token_ids, cu_seqlens, total_tokens,
+    return (_lib or lib()).elis_logits_adjust(logits, dtype, in_stride, n, vocab, token_ids, cu_seqlens, total_tokens,
                                     prompt_lens, repetition, frequency, presence, bias_cu, bias_tokens, bias_values,
                                     bias_total, mask, n_masks, mask_stride, mask_rows, out, out_stride, stream)
 

@@ -212,6 +212,7 @@ struct KvAttnArgs {
     int nchunks, chunk, small, small_rows;
     float* part_o;
     float2* part_ml;
+    size_t many_parts_at;  // one launch for both kinds of requests: where the long ones' chunk results begin
 };
 // Row of the chunk results that (request, kv head, row) or (token, head) has.
 __device__ __forceinline__ size_t part_row(const KvAttnArgs& a, bool many, int req, int h, int tok, int head, int r) {

@@ -15,7 +15,7 @@
 // Softmax: running maximum and sum in fp32; the maximum lags: the accumulators are rescaled only when a score exceeds it
 // by 2^8, which each lane can tell from its own scores, so the lanes of a row exchange theirs only then. It is kept as a
 // whole number of powers of two, so that rescaling is exact, that of weights in bf16 too. The weights are
-// rounded to bf16 for the second product (half a step, 2^-8 of each); their sum is not.
+// rounded to bf16 for the second product (half a step, 2^-8 of each), and the rounded ones are summed.
 //
 // Masks. A key is seen when it is at or before the token's position, inside its window, and on a valid page. Records
 // wholly seen by every row skip the test. The codes of keys that no row may see (past the end, on a bad page) are
@@ -35,10 +35,8 @@ namespace {
 constexpr int kStep = 32;  // keys a wave takes at a time: two records
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
+constexpr unsigned kMixedMost = 2048;  // work-groups of short requests up to which they run beside the long ones'
 constexpr float kLowest = -3.0e38f;  // a maximum over no keys: finite, so that differences of maxima are numbers
-#ifndef XOCC
-#define XOCC 3
-#endif
 constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
 
 // Maxima as single instructions: fmaxf first quiets each operand's signalling NaN with an instruction of its own.
@@ -51,6 +49,16 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
     return r;
+}
+
+// s + both halves of w, a pair of bf16.
+__device__ __forceinline__ float dot2(uint32_t w, float s) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), s, false);
+#else
+    return s;
+#endif
 }
 
 // Maximum over the lanes l, l^16, l^32, l^48, which hold one row's scores.
@@ -114,8 +122,7 @@ __device__ __forceinline__ int chunks_of(int lo, int hi, int chunk) {
 // Tile `want` of TILE rows among the requests with more than a.small rows, by all kThreads threads of the work-group (the
 // two results are in LDS); false if there are fewer.
 template <int TILE>
-__device__ __forceinline__ bool find_tile(const KvAttnArgs& a, int want, int* req, int* rt) {
-    __shared__ int tot[kWaves];
+__device__ __forceinline__ bool find_tile(const KvAttnArgs& a, int want, int* tot, int* req, int* rt) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = tid / kWave;
     int before = 0;
     for (int base = 0; base < a.n; base += kThreads) {
@@ -160,22 +167,33 @@ __device__ __forceinline__ float scale_of(uint32_t dword, int byte) {
     return __uint_as_float(((dword >> (8 * byte)) & 0xFFu) << 23);
 }
 
-// MANY: rows of every request with more than `small` rows, in tiles; else the others, one tile each.
+// LDS of a work-group.
+template <int D, int NB>
+struct Shared {
+    static constexpr bool kQueries = NB == 4;  // 64 query rows in LDS: their registers are what a second wave on the SIMD needs
+    bf16x8 q[kQueries ? NB * (D / 32) * kWave : 1];
+    float o[kWaves][16][D + 4];
+    float m[kWaves][NB * 16], l[kWaves][NB * 16];
+    int tot[kWaves], req, rt;
+};
+
+// One work-group's part, number `unit`. MANY: rows of every request with more than `small` rows, in tiles; else the
+// others, one tile each.
 template <int D, int NB, bool MANY>
-__global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_kernel(KvAttnArgs a) {
+__device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Shared<D, NB>& sh) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using R = Rec<D>;
     typedef typename RecRegs<D>::vec vec;
     constexpr int KS = D / 32;   // k-steps of the first product
     constexpr int DB = D / 16;   // 16-row blocks of O^T; values of a column
-    constexpr bool QLDS = NB == 4;  // 64 query rows in LDS: their registers are what a second wave on the SIMD needs
-    __shared__ __attribute__((aligned(16))) float so[kWaves][16][D + 4];
-    __shared__ float sm[kWaves][NB * 16], sl[kWaves][NB * 16];
-    __shared__ __attribute__((aligned(16))) bf16x8 sq[QLDS ? NB * KS * kWave : 1];
+    constexpr bool QLDS = Shared<D, NB>::kQueries;
+    auto& so = sh.o;
+    auto& sm = sh.m;
+    auto& sl = sh.l;
+    auto& sq = sh.q;
 
     // Heads fastest, then requests, tiles and chunks: the work-groups of one chunk number, which only long requests
     // have many of, spread over all XCDs (with chunks fastest 8 of them put every first chunk on one XCD: 48 -> 25 us).
-    unsigned unit = blockIdx.x;
     const int h = static_cast<int>(unit % a.c.n_kv_heads);
     unit /= a.c.n_kv_heads;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -183,11 +201,10 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
     int req, rt = 0, chunk_i;
     if constexpr (MANY) {
         // Tiles are numbered through the requests that have more than `small` rows, last tile (most keys) first.
-        __shared__ int found_req, found_rt;
         chunk_i = static_cast<int>(unit % a.nchunks);
-        if (!find_tile<NB * 16>(a, static_cast<int>(unit / a.nchunks), &found_req, &found_rt)) return;
-        req = found_req;
-        rt = found_rt;
+        if (!find_tile<NB * 16>(a, static_cast<int>(unit / a.nchunks), sh.tot, &sh.req, &sh.rt)) return;
+        req = sh.req;
+        rt = sh.rt;
     } else {
         req = static_cast<int>(unit % a.n);
         chunk_i = static_cast<int>(unit / a.n);
@@ -340,6 +357,9 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
         // Uniform: some key of the step is not seen by some row.
         const bool edge = kb + kStep > all_hi || kb < all_lo || !there[0] || !there[1];
         uint32_t pw[NB][4];  // the weights, as the second product's operand
+        // Of two waves on a SIMD the one that multiplies goes first: the other's exponentials fill in behind (498 -> 466 us
+        // for 2,048 tokens over 16,000).
+        if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int u0 = 0; u0 < 2; u0 += UB) {
             f32x4 s[UB][NB];
@@ -365,23 +385,26 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
                         s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), q[j], s[u][j], 0, 0, 0);
                 }
             }
+            if constexpr (INPLACE) __builtin_amdgcn_s_setprio(0);
             if (edge) {
-                int pos[NB], from[NB];
+                int from[NB];        // row c of block j sees the keys from, from + 1, ..., from + more; none: from lies past all
+                uint32_t more[NB];
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    pos[j] = back + token(j);
-                    from[j] = a.window > 0 ? pos[j] - a.window + 1 : 0;
+                    const int pos = back + token(j), f = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+                    from[j] = pos < 0 ? INT32_MAX : f;
+                    more[j] = pos < 0 ? 0u : static_cast<uint32_t>(pos - f);
                 }
 #pragma unroll
                 for (int u = 0; u < UB; ++u) {
-                    const int v = u0 + u, kv = kb + 16 * v;
+                    const int v = u0 + u, kv = there[v] ? kb + 16 * v : INT32_MIN;  // a record that is not there: before all keys
                     uint32_t nan = 0u;  // of this lane's four keys, those whose values are NaN
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = kv + 4 * g + i;
 #pragma unroll
                         for (int j = 0; j < NB; ++j)
-                            if (!there[v] || key > pos[j] || key < from[j]) s[u][j][i] = -INFINITY;
+                            if (static_cast<uint32_t>(key) - static_cast<uint32_t>(from[j]) > more[j]) s[u][j][i] = -INFINITY;
                         // values that no row may see, or that are NaN, multiply as zero
                         const bool is_nan = ((x.vs[v] >> (8 * i)) & 0xFFu) == 0xFFu;
                         if (is_nan) {
@@ -402,7 +425,7 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
                             const uint32_t w = __shfl(nan, (y >> 2) * 16 + from_c, kWave);
 #pragma unroll
                             for (int j = 0; j < NB; ++j)
-                                if (((w >> (y & 3)) & 1u) && kv + y <= pos[j] && kv + y >= from[j]) {
+                                if (((w >> (y & 3)) & 1u) && static_cast<uint32_t>(kv + y) - static_cast<uint32_t>(from[j]) <= more[j]) {
 #pragma unroll
                                     for (int b = 0; b < DB; ++b) o[b][j] = f32x4{NAN, NAN, NAN, NAN};
                                 }
@@ -417,7 +440,12 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
             for (int j = 0; j < NB; ++j) {
                 t[j] = max2(max3(s[0][j][0], s[0][j][1], s[0][j][2]), s[0][j][3]);
                 if constexpr (UB == 2) t[j] = max3(t[j], max3(s[1][j][0], s[1][j][1], s[1][j][2]), s[1][j][3]);
-                over = max2(over, fmaf(t[j], sc, -m[j]));
+            }
+#pragma unroll
+            for (int j = 0; j < NB; j += 2) {
+                const float x0 = fmaf(t[j], sc, -m[j]);
+                if (j + 1 < NB) over = max3(over, x0, fmaf(t[(j + 1) % NB], sc, -m[(j + 1) % NB]));
+                else over = x0;
             }
             if (__ballot(over > 8.f) != 0ull) {
 #pragma unroll
@@ -444,14 +472,16 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][j][i], sc, -m[j]));
-                    lsum[j] += (p[0] + p[1]) + (p[2] + p[3]);
-                    pw[j][2 * (u0 + u)] = pack_bf16x2(p[0], p[1]);
-                    pw[j][2 * (u0 + u) + 1] = pack_bf16x2(p[2], p[3]);
+                    const uint32_t w0 = pack_bf16x2(p[0], p[1]), w1 = pack_bf16x2(p[2], p[3]);
+                    pw[j][2 * (u0 + u)] = w0;
+                    pw[j][2 * (u0 + u) + 1] = w1;
+                    lsum[j] = dot2(w1, dot2(w0, lsum[j]));
                 }
         }
         bf16x8 pf[NB];
 #pragma unroll
         for (int j = 0; j < NB; ++j) pf[j] = __builtin_bit_cast(bf16x8, u32x4{pw[j][0], pw[j][1], pw[j][2], pw[j][3]});
+        if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
         // V^T: for every pair of a column's values, the eight keys' pairs, then even and odd value as operands of two blocks
         float vsc[8];
 #pragma unroll
@@ -564,6 +594,32 @@ __global__ __launch_bounds__(kThreads, NB == 1 ? XOCC : 2) void kv_attention_ker
 #endif
 }
 
+template <int D, int NB, bool MANY>
+__global__ __launch_bounds__(kThreads, NB == 1 ? 4 : 2) void kv_attention_kernel(KvAttnArgs a) {
+    __shared__ __attribute__((aligned(16))) Shared<D, NB> sh;
+    attend<D, NB, MANY>(a, blockIdx.x, sh);
+}
+
+// Both at once, the long requests' tiles first: neither waits for the other's last work-groups.
+template <int D, int NB>
+__global__ __launch_bounds__(kThreads, 2) void kv_attention_mixed_kernel(KvAttnArgs a, int many_units, int many_chunk, int many_nchunks) {
+    union Both {
+        Shared<D, 4> many;
+        Shared<D, NB> small;
+    };
+    __shared__ __attribute__((aligned(16))) char raw[sizeof(Both)];
+    Both& sh = *reinterpret_cast<Both*>(raw);
+    if (blockIdx.x < static_cast<unsigned>(many_units)) {
+        a.chunk = many_chunk;
+        a.nchunks = many_nchunks;
+        a.part_o += a.many_parts_at * D;
+        a.part_ml += a.many_parts_at;
+        attend<D, 4, true>(a, blockIdx.x, sh.many);
+    } else {
+        attend<D, NB, false>(a, blockIdx.x - many_units, sh.small);
+    }
+}
+
 // Joins the chunks of split rows, in an order that depends on their number alone. WAVES waves a row, each taking every
 // WAVES-th chunk: with one wave a row of 118 chunks took 38 us, its loads one behind the other.
 template <int D, bool MANY, int WAVES>
@@ -654,22 +710,29 @@ hipError_t combine(const KvAttnArgs& a, long long rows, int rows_per, int tile, 
 
 template <int D>
 hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
-    KvAttnArgs a = args;
-    const unsigned per = static_cast<unsigned>(a.c.n_kv_heads) * a.n;
-    if (p.small_rows > 0) {
-        a.nchunks = p.small_chunks;
-        a.chunk = p.small_chunk;
-        const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : p.small_nb == 2 ? kv_attention_kernel<D, 2, false> : kv_attention_kernel<D, 4, false>;
-        ELIS_TRY(launch_kernel(f, dim3(per * p.small_chunks), dim3(kThreads), 0, st, a));
-        if (p.small_chunks > 1)
-            ELIS_TRY((combine<D, false>(a, static_cast<long long>(per) * p.small_rows, p.small_rows, 16 * p.small_nb, st)));
+    KvAttnArgs a = args, b = args;  // of the short requests, of the long ones
+    const unsigned small = p.small_rows > 0 ? static_cast<unsigned>(a.c.n_kv_heads) * a.n * p.small_chunks : 0;
+    const unsigned many = p.many_tiles > 0 ? static_cast<unsigned>(a.c.n_kv_heads) * p.many_tiles * p.many_chunks : 0;
+    a.nchunks = p.small_chunks;
+    a.chunk = p.small_chunk;
+    b.nchunks = p.many_chunks;
+    b.chunk = p.many_chunk;
+    b.part_o += p.small_parts * D;  // both may have chunk results at once
+    b.part_ml += p.small_parts;
+    if (small && many && small <= kMixedMost) {
+        const auto f = p.small_nb == 1 ? kv_attention_mixed_kernel<D, 1> : p.small_nb == 2 ? kv_attention_mixed_kernel<D, 2> : kv_attention_mixed_kernel<D, 4>;
+        a.many_parts_at = p.small_parts;
+        ELIS_TRY(launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, static_cast<int>(many), p.many_chunk, p.many_chunks));
+    } else {
+        if (small) {
+            const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : p.small_nb == 2 ? kv_attention_kernel<D, 2, false> : kv_attention_kernel<D, 4, false>;
+            ELIS_TRY(launch_kernel(f, dim3(small), dim3(kThreads), 0, st, a));
+        }
+        if (many) ELIS_TRY(launch_kernel(kv_attention_kernel<D, 4, true>, dim3(many), dim3(kThreads), 0, st, b));
     }
-    if (p.many_tiles > 0) {
-        a.nchunks = p.many_chunks;
-        a.chunk = p.many_chunk;
-        ELIS_TRY(launch_kernel(kv_attention_kernel<D, 4, true>, dim3(static_cast<unsigned>(a.c.n_kv_heads) * p.many_tiles * p.many_chunks), dim3(kThreads), 0, st, a));
-        if (p.many_chunks > 1) ELIS_TRY((combine<D, true>(a, static_cast<long long>(a.total_q) * a.n_heads, 0, 64, st)));
-    }
+    if (small && p.small_chunks > 1)
+        ELIS_TRY((combine<D, false>(a, static_cast<long long>(a.c.n_kv_heads) * a.n * p.small_rows, p.small_rows, 16 * p.small_nb, st)));
+    if (many && p.many_chunks > 1) ELIS_TRY((combine<D, true>(b, static_cast<long long>(a.total_q) * a.n_heads, 0, 64, st)));
     return hipSuccess;
 }
 

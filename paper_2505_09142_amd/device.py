@@ -204,16 +204,20 @@ def _opt(t: torch.Tensor | None, dtype: torch.dtype, dev: int, where: str, at_le
     return None if t is None else _arg(t, dtype, dev, where, at_least)
 
 
-def _heads(x: torch.Tensor, heads: int, d: int, dev: int, where: str) -> int:
+def _heads(x: torch.Tensor, tokens: int, heads: int, d: int, dev: int, where: str) -> int:
     """Token stride of a [tokens, heads, d] or [tokens, heads * d] bf16 tensor whose rows are contiguous."""
-    shape = x.shape
-    if len(shape) == 3:
-        ok = shape[1] == heads and shape[2] == d and (heads == 1 or x.stride(1) == d)
-    else:
-        ok = len(shape) == 2 and shape[1] == heads * d
-    if not ok or x.dtype is not torch.bfloat16 or x.get_device() != dev or x.stride(-1) != 1:
+    if x.dtype is not torch.bfloat16 or x.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
-    return x.stride(0) if shape[0] > 1 else heads * d
+    shape, stride = x.shape, x.stride()
+    if shape == (tokens, heads, d):
+        if stride[2] == 1 and (heads == 1 or stride[1] == d):
+            return stride[0] if tokens > 1 else heads * d
+    elif shape == (tokens, heads * d):
+        if stride[1] == 1:
+            return stride[0] if tokens > 1 else heads * d
+    else:
+        raise E.ElisError(E.ELIS_ESHAPE, where)
+    raise E.ElisError(E.ELIS_EINVAL, where)
 
 
 class PagePool:
@@ -298,9 +302,8 @@ class KVCache:
         """bf16 [tokens, n_kv_heads, d_head] (rows of a wider matrix are taken as they are) into their slots."""
         n, where = slot_map.numel(), "elis_kv_append"
         dev = self._here(where)
-        ks, vs = _heads(k, self.n_kv_heads, self.d_head, dev, where), _heads(v, self.n_kv_heads, self.d_head, dev, where)
-        if k.shape[0] != n or v.shape[0] != n:
-            raise E.ElisError(E.ELIS_ESHAPE, where)
+        ks = _heads(k, n, self.n_kv_heads, self.d_head, dev, where)
+        vs = _heads(v, n, self.n_kv_heads, self.d_head, dev, where)
         E.check(E.elis_kv_append(self.c, k.data_ptr(), v.data_ptr(), ks, vs, _arg(slot_map, torch.int32, dev, where), n,
                                  _stream(stream)), where)
 
@@ -308,10 +311,8 @@ class KVCache:
         """What the cache keeps of the tokens in slot_map, as bf16."""
         n, where = slot_map.numel(), "elis_kv_read"
         dev = self._here(where)
-        ks = _heads(out_k, self.n_kv_heads, self.d_head, dev, where)
-        vs = _heads(out_v, self.n_kv_heads, self.d_head, dev, where)
-        if out_k.shape[0] != n or out_v.shape[0] != n:
-            raise E.ElisError(E.ELIS_ESHAPE, where)
+        ks = _heads(out_k, n, self.n_kv_heads, self.d_head, dev, where)
+        vs = _heads(out_v, n, self.n_kv_heads, self.d_head, dev, where)
         E.check(E.elis_kv_read(self.c, _arg(slot_map, torch.int32, dev, where), n, out_k.data_ptr(), out_v.data_ptr(), ks, vs,
                                _stream(stream)), where)
 
@@ -322,21 +323,20 @@ class KVCache:
         row of page ids for every request, or, with ``rows``, for every job slot (a pool's table)."""
         n, i32, where = kv_lens.numel(), torch.int32, "elis_kv_attention"
         dev = self._here(where)
-        if q.dim() != 3 or blocks.dim() != 2 or q.shape[2] != self.d_head:
+        if q.dim() != 3 or blocks.dim() != 2:
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        total, heads = q.shape[0], q.shape[1]
+        total, heads, d = q.shape[0], q.shape[1], self.d_head
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        qs, os_ = _heads(q, heads, self.d_head, dev, where), _heads(out, heads, self.d_head, dev, where)
-        if out.shape[0] != total:
-            raise E.ElisError(E.ELIS_ESHAPE, where)
+            out = torch.empty((total, heads, d), dtype=torch.bfloat16, device=q.device)
+        qs, os_ = _heads(q, total, heads, d, dev, where), _heads(out, total, heads, d, dev, where)
+        block_rows, block_cols = blocks.shape
         sizes = (n, total, max_q, max_kv, heads)
         if sizes != self._sizes:
             self._need = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, self.d_head)
             self._sizes = sizes
         ws, wsb = self.ws.get(self._need)
         E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, dev, where, n + 1), n, total, max_q,
-                                    _arg(blocks, i32, dev, where), blocks.shape[0], blocks.shape[1],
+                                    _arg(blocks, i32, dev, where), block_rows, block_cols,
                                     _opt(rows, i32, dev, where, n), _arg(kv_lens, i32, dev, where), max_kv, heads,
                                     self.d_head ** -0.5 if scale is None else scale, window, out.data_ptr(), os_, ws, wsb,
                                     _stream(stream)), where)
