@@ -289,7 +289,7 @@ class KVCache:
         self.buf, self.dev = buf, buf.get_device()
         self.c = E.elis_kv_cache(base, n_pages, page_tokens, n_kv_heads, d_head)
         self.ws = Workspace(buf.device)
-        self._sizes, self._need = None, 0  # of the last attention call: its sizes and their workspace
+        self._sizes, self._ws = None, (0, 0)  # of the last attention call: its sizes, and the workspace they take
         if made:
             E.check(E.elis_kv_init(self.c, _stream(stream)), "elis_kv_init")
 
@@ -325,16 +325,17 @@ class KVCache:
         dev = self._here(where)
         if q.dim() != 3 or blocks.dim() != 2:
             raise E.ElisError(E.ELIS_ESHAPE, where)
-        total, heads, d = q.shape[0], q.shape[1], self.d_head
+        total, heads, _ = q.shape
+        d = self.d_head
         if out is None:
             out = torch.empty((total, heads, d), dtype=torch.bfloat16, device=q.device)
         qs, os_ = _heads(q, total, heads, d, dev, where), _heads(out, total, heads, d, dev, where)
         block_rows, block_cols = blocks.shape
         sizes = (n, total, max_q, max_kv, heads)
         if sizes != self._sizes:
-            self._need = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, self.d_head)
+            self._ws = self.ws.get(E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d))
             self._sizes = sizes
-        ws, wsb = self.ws.get(self._need)
+        ws, wsb = self._ws
         E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, dev, where, n + 1), n, total, max_q,
                                     _arg(blocks, i32, dev, where), block_rows, block_cols,
                                     _opt(rows, i32, dev, where, n), _arg(kv_lens, i32, dev, where), max_kv, heads,

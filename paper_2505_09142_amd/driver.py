@@ -12,7 +12,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from .device import JobTable, Predictor
+from .device import JobTable, PagePool, Predictor, adjust_logits
 
 
 def build_input(prompt: np.ndarray, response: np.ndarray, generated: int, max_pos: int) -> np.ndarray:
@@ -117,9 +117,16 @@ class DeviceRoundDriver:
     predictions in the table, and selects over the cached predictions of the
     candidates; the chosen slots are the round's only device-to-host transfer.
     Every upload of a call goes through one pinned staging buffer in one copy.
+
+    With ``pages`` (a PagePool with a slot for every job slot) a job's table slot is its
+    slot of the pool too: reserve() gives the chosen jobs pages of the served model's KV
+    cache, drop() takes a preempted job's back, and release() a finished one's.
     """
 
-    def __init__(self, predictor: Predictor, max_jobs: int, max_pos: int, device="cuda"):
+    def __init__(self, predictor: Predictor, max_jobs: int, max_pos: int, device="cuda", pages: PagePool | None = None):
+        if pages is not None and pages.max_jobs < max_jobs:
+            raise ValueError("the page pool has fewer job slots than the table")
+        self.pages = pages
         self.pr = predictor
         self.max_jobs, self.max_pos = max_jobs, max_pos
         self.device = device
@@ -176,7 +183,9 @@ class DeviceRoundDriver:
         return out
 
     def release(self, jobs):
-        """Jobs that finished give their slots back."""
+        """Jobs that finished give their slots back, and their pages."""
+        if self.pages is not None:
+            self.drop(jobs)
         for j in jobs:
             s = self.slot_of.pop(j)
             self.job_of[s] = -1
@@ -197,6 +206,55 @@ class DeviceRoundDriver:
         slots = np.array([self.slot_of[j] for j in jobs], dtype=np.int32)
         d_slots, d_arr = self._upload(slots, np.asarray(arrival_seq, dtype=np.int64))
         self.table.start(d_slots, d_arr)
+
+    def _slots(self, jobs) -> np.ndarray:
+        return np.fromiter((self.slot_of[j] for j in jobs), dtype=np.int32, count=len(jobs))
+
+    def reserve(self, jobs, lens, new=None, out_slot_map: torch.Tensor | None = None,
+                out_blocks: torch.Tensor | None = None) -> torch.Tensor:
+        """Pages for the jobs' lens tokens, in the order of the call (the selection's: the first jobs are served first
+        when pages run out). With `new`, the last new[i] of job i's tokens are this step's: their cache slots go into
+        out_slot_map. Returns the jobs' slots, the rows of the pool's table, on the device (valid until the next call)."""
+        cu = np.zeros(len(jobs) + 1, dtype=np.int32)
+        if new is not None:
+            np.cumsum(new, out=cu[1:])
+        d_slots, d_lens, d_cu = self._upload(self._slots(jobs), np.asarray(lens, dtype=np.int32), cu)
+        self.pages.grow(d_slots, d_lens, d_cu, int(cu[-1]), out_slot_map, out_blocks=out_blocks)
+        return d_slots
+
+    def drop(self, jobs):
+        """Jobs that were preempted or have finished give their pages back."""
+        if len(jobs) == 0:
+            return
+        d_slots, d_lens = self._upload(self._slots(jobs), np.zeros(len(jobs), dtype=np.int32))
+        self.pages.trim(d_slots, d_lens)
+
+    def adjust_logits(self, jobs, logits: torch.Tensor, prompt_lens, out: torch.Tensor | None = None, **kw) -> torch.Tensor:
+        """device.adjust_logits on one row of logits a job, with the tokens that the table holds as its history (past
+        max_pos tokens the first one and the most recent max_pos - 1). The other arguments are passed on."""
+        n = len(jobs)
+        if logits.dim() != 2 or logits.shape[0] != n:
+            raise ValueError("one row of logits for each job")
+        if n == 0:
+            return adjust_logits(logits, None, None, out)
+        total = np.fromiter((self.appended[j] for j in jobs), dtype=np.int64, count=n)
+        held = np.minimum(total, self.max_pos)
+        # of a longer history the first token and those from `tail` on are held: so many of them are the prompt's
+        plen, tail = np.asarray(prompt_lens, dtype=np.int64), total - (self.max_pos - 1)
+        seen = np.where(total <= self.max_pos, plen, np.minimum(plen, 1) + np.maximum(plen - tail, 0))
+        T = int(held.sum())
+        ids, cu = self._buffers(T, n)
+        d_slots, d_seen = self._upload(self._slots(jobs), seen.astype(np.int32))
+        self.table.pack(d_slots, T, int(held.max()), ids, cu)
+        return adjust_logits(logits, ids, cu, out, prompt_lens=d_seen, **kw)
+
+    def _buffers(self, T: int, n: int):
+        """Packed token ids and offsets of n jobs with T tokens (views of buffers that grow on demand)."""
+        if self._ids.numel() < T:
+            self._ids = torch.empty(max(T, 2 * self._ids.numel()), dtype=torch.int32, device=self.device)
+        if self._cu.numel() < n + 1:
+            self._cu = torch.empty(max(n + 1, 2 * self._cu.numel()), dtype=torch.int32, device=self.device)
+        return self._ids[:T], self._cu[:n + 1]
 
     def sync_tokens(self, jobs, prompts, responses, generated):
         """Appends to each job the tokens it gained since its last append: the prompt when it
@@ -227,12 +285,8 @@ class DeviceRoundDriver:
         returns them as a device tensor (no synchronisation)."""
         lens = np.fromiter((min(self.appended[j], self.max_pos) for j in jobs), dtype=np.int64, count=len(jobs))
         T, n, mx = int(lens.sum()), len(jobs), int(lens.max())
-        if self._ids.numel() < T:
-            self._ids = torch.empty(max(T, 2 * self._ids.numel()), dtype=torch.int32, device=self.device)
-        if self._cu.numel() < n + 1:
-            self._cu = torch.empty(max(n + 1, 2 * self._cu.numel()), dtype=torch.int32, device=self.device)
-        (d_slots,) = self._upload(np.fromiter((self.slot_of[j] for j in jobs), dtype=np.int32, count=n))
-        ids, cu = self._ids[:T], self._cu[:n + 1]
+        ids, cu = self._buffers(T, n)
+        (d_slots,) = self._upload(self._slots(jobs))
         self.table.pack(d_slots, T, mx, ids, cu)
         pred, _ = self.pr.predict(ids, cu, mx, out_pred=out_pred)
         self.table.store_pred(d_slots, pred)

@@ -25,7 +25,10 @@ Starvation control and preemption cost (Sec. 3.4 leaves both open):
                 the window waits for it.
 
 The round driver (DeviceRoundDriver or HostRoundDriver) owns the predictor,
-the key cache and the selection; the loop itself is host bookkeeping only.
+the key cache and the selection; the loop itself is host bookkeeping only. With
+a page pool (DeviceRoundDriver's `pages`) the chosen jobs hold the KV pages of
+their prompt and of the tokens they will have at the window's end; preempted and
+finished jobs give theirs back.
 """
 from __future__ import annotations
 
@@ -80,6 +83,7 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
     last_batch: list = []
     next_arrival, finished, now = 0, 0, 0.0
     use_encoder = policy == "isrtf" and key_fn is None
+    pages = getattr(driver, "pages", None) is not None
     out = ScheduleResult()
     while finished < n and (max_rounds is None or len(out.rounds) < max_rounds):
         fresh = []
@@ -117,10 +121,10 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
         chosen = [int(j) for j in driver.select(candidates, batch_cap, wait=wait, aging=aging)]
         latency = time.perf_counter() - t0
         in_batch = set(chosen)
-        for j in last_batch:
-            if j not in in_batch:
-                dropped[j] = True
-                preempted[j] += 1
+        gone = [j for j in last_batch if j not in in_batch]
+        for j in gone:
+            dropped[j] = True
+            preempted[j] += 1
         resumed = sorted(j for j in chosen if dropped[j])
         prefill_s = prefill_cost * sum(int(plen[j] + gen[j]) for j in resumed) if resumed else 0.0
         dropped[resumed] = False
@@ -131,6 +135,9 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
             steps = min(budget.values())
         else:
             raise ValueError(end_rule)
+        if pages:
+            driver.drop(gone)
+            driver.reserve(chosen, [int(plen[j] + gen[j]) + min(budget[j], steps) for j in chosen])
         end = now + prefill_s + steps * step_cost
         done_now = []
         last_batch = []
