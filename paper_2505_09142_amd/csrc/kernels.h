@@ -183,15 +183,17 @@ hipError_t launch_kv_append(KvCacheView c, const uint16_t* k, const uint16_t* v,
 hipError_t launch_kv_read(KvCacheView c, const int32_t* map, int n, uint16_t* k, uint16_t* v, long long k_stride, long long v_stride, hipStream_t st);
 
 // kv_attention.hip
-// Launches of one call: requests of up to `small` rows (new tokens x heads of a group) in tiles of 16 small_nb rows
-// and chunks of small_chunk keys, longer ones in tiles of their own.
+// Launches of one call: requests of up to `small` rows (new tokens x heads of a group) in one tile of 16 small_nb rows and
+// chunks of small_chunk keys, longer ones in tiles of 16 many_nb rows.
 struct KvAttnPlan {
     int small, small_nb, small_rows, small_chunk, small_chunks;
     bool many;
-    int many_tiles, many_chunk, many_chunks;
+    int many_nb, many_tiles, many_chunk, many_chunks;
+    long long small_most, many_most;  // chunks at most, with any window
     size_t small_parts, many_parts;  // chunk results to join (d_head floats and two more each)
 };
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads);
+KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int window);
+long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads);
 struct KvAttnArgs {
     KvCacheView c;
     const uint16_t* q;
@@ -212,7 +214,18 @@ struct KvAttnArgs {
     int nchunks, chunk, small, small_rows;
     float* part_o;
     float2* part_ml;
-    size_t many_parts_at;  // one launch for both kinds of requests: where the long ones' chunk results begin
+};
+// What differs for the requests of many rows.
+struct KvAttnMany {
+    int units, chunk, nchunks, tile;
+    size_t parts_at;  // where their chunk results begin
+    __host__ __device__ KvAttnArgs of(KvAttnArgs a, int d) const {
+        a.chunk = chunk;
+        a.nchunks = nchunks;
+        a.part_o += parts_at * d;
+        a.part_ml += parts_at;
+        return a;
+    }
 };
 // Row of the chunk results that (request, kv head, row) or (token, head) has.
 __device__ __forceinline__ size_t part_row(const KvAttnArgs& a, bool many, int req, int h, int tok, int head, int r) {

@@ -170,7 +170,7 @@ __device__ __forceinline__ float scale_of(uint32_t dword, int byte) {
 // LDS of a work-group.
 template <int D, int NB>
 struct Shared {
-    static constexpr bool kQueries = NB == 4;  // 64 query rows in LDS: their registers are what a second wave on the SIMD needs
+    static constexpr bool kQueries = NB > 1;  // many query rows in LDS: their registers are what another wave on the SIMD needs
     bf16x8 q[kQueries ? NB * (D / 32) * kWave : 1];
     float o[kWaves][16][D + 4];
     float m[kWaves][NB * 16], l[kWaves][NB * 16];
@@ -316,9 +316,11 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
         }
     }
     if constexpr (QLDS) {
-        static_assert(NB == kWaves, "a block of rows a wave");
+        static_assert(NB <= kWaves, "a block of rows a wave");
+        if (wid < NB) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) sq[(wid * KS + s) * kWave + lane] = qf[0][s];
+            for (int s = 0; s < KS; ++s) sq[(wid * KS + s) * kWave + lane] = qf[0][s];
+        }
         __syncthreads();
     }
     auto query = [&](int j, int s) { return QLDS ? sq[(j * KS + s) * kWave + lane] : qf[QLDS ? 0 : j][s]; };
@@ -594,42 +596,45 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
 #endif
 }
 
+constexpr int waves_per_simd(int nb) { return nb == 1 ? 4 : nb == 2 ? 3 : 2; }
+
 template <int D, int NB, bool MANY>
-__global__ __launch_bounds__(kThreads, NB == 1 ? 4 : 2) void kv_attention_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kThreads, waves_per_simd(NB)) void kv_attention_kernel(KvAttnArgs a) {
     __shared__ __attribute__((aligned(16))) Shared<D, NB> sh;
     attend<D, NB, MANY>(a, blockIdx.x, sh);
 }
 
 // Both at once, the long requests' tiles first: neither waits for the other's last work-groups.
-template <int D, int NB>
-__global__ __launch_bounds__(kThreads, 2) void kv_attention_mixed_kernel(KvAttnArgs a, int many_units, int many_chunk, int many_nchunks) {
+template <int D, int NB, int NBM>
+__global__ __launch_bounds__(kThreads, waves_per_simd(NBM)) void kv_attention_mixed_kernel(KvAttnArgs a, KvAttnMany m) {
     union Both {
-        Shared<D, 4> many;
+        Shared<D, NBM> many;
         Shared<D, NB> small;
     };
     __shared__ __attribute__((aligned(16))) char raw[sizeof(Both)];
     Both& sh = *reinterpret_cast<Both*>(raw);
-    if (blockIdx.x < static_cast<unsigned>(many_units)) {
-        a.chunk = many_chunk;
-        a.nchunks = many_nchunks;
-        a.part_o += a.many_parts_at * D;
-        a.part_ml += a.many_parts_at;
-        attend<D, 4, true>(a, blockIdx.x, sh.many);
+    if (blockIdx.x < static_cast<unsigned>(m.units)) {
+        attend<D, NBM, true>(m.of(a, D), blockIdx.x, sh.many);
     } else {
-        attend<D, NB, false>(a, blockIdx.x - many_units, sh.small);
+        attend<D, NB, false>(a, blockIdx.x - m.units, sh.small);
     }
 }
 
 // Joins the chunks of split rows, in an order that depends on their number alone. WAVES waves a row, each taking every
 // WAVES-th chunk: with one wave a row of 118 chunks took 38 us, its loads one behind the other.
-template <int D, bool MANY, int WAVES>
-__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int rows_per, int tile) {
+// The first small_units rows are those of short requests (a.small_rows each), then comes one for each token and head.
+template <int D, int WAVES>
+__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAttnMany m, long long small_units, int small_tile) {
     __shared__ __attribute__((aligned(16))) float part[WAVES > 1 ? kWaves : 1][D];
     const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
-    const long long w = static_cast<long long>(blockIdx.x) * (kWaves / WAVES) + wid / WAVES;
+    long long w = static_cast<long long>(blockIdx.x) * (kWaves / WAVES) + wid / WAVES;
     const int wi = wid % WAVES;
+    const bool many = w >= small_units;
+    const int tile = many ? m.tile : small_tile;
     int req, h, r;
-    if constexpr (MANY) {
+    if (many) {
+        w -= small_units;
+        a = m.of(a, D);
         const long long tok = w / a.n_heads;
         if (tok >= a.total_q) return;
         const int head = static_cast<int>(w - tok * a.n_heads);
@@ -637,22 +642,22 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int 
         h = head / a.group;
         r = static_cast<int>(tok - a.cu[req]) * a.group + (head - h * a.group);
     } else {
-        r = static_cast<int>(w % rows_per);
-        const long long u = w / rows_per;
+        r = static_cast<int>(w % a.small_rows);
+        const long long u = w / a.small_rows;
         h = static_cast<int>(u % a.c.n_kv_heads);
         if (u / a.c.n_kv_heads >= a.n) return;
         req = static_cast<int>(u / a.c.n_kv_heads);
     }
     const Request rq = request_of(a, req);
     const int rows = rq.ql * a.group;
-    if (!rq.ok || r < 0 || r >= rows || (MANY ? rows <= a.small : rows > a.small)) return;
+    if (!rq.ok || r < 0 || r >= rows || (many ? rows <= a.small : rows > a.small)) return;
     const int r0 = r / tile * tile, r1 = r0 + tile < rows ? r0 + tile : rows;
     int lo, hi;
     span_of(a, rq, r0, r1, &lo, &hi);
     const int nc = chunks_of(lo, hi, a.chunk);
     if (nc == 1) return;  // every return is the same for the waves of a row
     const int t = r / a.group, head = h * a.group + (r - t * a.group);
-    const size_t at = part_row(a, MANY, req, h, rq.q0 + t, head, r) * a.nchunks;
+    const size_t at = part_row(a, many, req, h, rq.q0 + t, head, r) * a.nchunks;
     constexpr int PL = D / kWave;  // values a lane
     constexpr int AHEAD = 8;       // chunks a wave fetches at a time, the first before their weights are known
     typedef float fvec __attribute__((ext_vector_type(PL)));
@@ -701,88 +706,104 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, int 
     for (int e = 0; e < PL; ++e) p[e] = f32_to_bf16(acc[e] * inv);
 }
 
-template <int D, bool MANY>
-hipError_t combine(const KvAttnArgs& a, long long rows, int rows_per, int tile, hipStream_t st) {
-    if (a.nchunks > 8)
-        return launch_kernel(kv_combine_kernel<D, MANY, kWaves>, dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, st, a, rows_per, tile);
-    return launch_kernel(kv_combine_kernel<D, MANY, 1>, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, rows_per, tile);
-}
-
 template <int D>
 hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
-    KvAttnArgs a = args, b = args;  // of the short requests, of the long ones
-    const unsigned small = p.small_rows > 0 ? static_cast<unsigned>(a.c.n_kv_heads) * a.n * p.small_chunks : 0;
-    const unsigned many = p.many_tiles > 0 ? static_cast<unsigned>(a.c.n_kv_heads) * p.many_tiles * p.many_chunks : 0;
+    KvAttnArgs a = args;  // as the short requests' launch takes it
     a.nchunks = p.small_chunks;
     a.chunk = p.small_chunk;
-    b.nchunks = p.many_chunks;
-    b.chunk = p.many_chunk;
-    b.part_o += p.small_parts * D;  // both may have chunk results at once
-    b.part_ml += p.small_parts;
+    const unsigned heads = static_cast<unsigned>(a.c.n_kv_heads);
+    const unsigned small = p.small_rows > 0 ? heads * a.n * p.small_chunks : 0, many = heads * p.many_tiles * p.many_chunks;
+    const KvAttnMany m{static_cast<int>(many), p.many_chunk, p.many_chunks, 16 * p.many_nb, p.small_parts};  // both may have chunk results at once
     if (small && many && small <= kMixedMost) {
-        const auto f = p.small_nb == 1 ? kv_attention_mixed_kernel<D, 1> : p.small_nb == 2 ? kv_attention_mixed_kernel<D, 2> : kv_attention_mixed_kernel<D, 4>;
-        a.many_parts_at = p.small_parts;
-        ELIS_TRY(launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, static_cast<int>(many), p.many_chunk, p.many_chunks));
+        const auto f = p.small_nb == 2 ? (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 2, 4> : kv_attention_mixed_kernel<D, 2, 2>)
+                                       : (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 1, 4> : kv_attention_mixed_kernel<D, 1, 2>);
+        ELIS_TRY(launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, m));
     } else {
         if (small) {
-            const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : p.small_nb == 2 ? kv_attention_kernel<D, 2, false> : kv_attention_kernel<D, 4, false>;
+            const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : kv_attention_kernel<D, 2, false>;
             ELIS_TRY(launch_kernel(f, dim3(small), dim3(kThreads), 0, st, a));
         }
-        if (many) ELIS_TRY(launch_kernel(kv_attention_kernel<D, 4, true>, dim3(many), dim3(kThreads), 0, st, b));
+        if (many) {
+            const auto f = p.many_nb == 2 ? kv_attention_kernel<D, 2, true> : kv_attention_kernel<D, 4, true>;
+            ELIS_TRY(launch_kernel(f, dim3(many), dim3(kThreads), 0, st, m.of(a, D)));
+        }
     }
-    if (small && p.small_chunks > 1)
-        ELIS_TRY((combine<D, false>(a, static_cast<long long>(a.c.n_kv_heads) * a.n * p.small_rows, p.small_rows, 16 * p.small_nb, st)));
-    if (many && p.many_chunks > 1) ELIS_TRY((combine<D, true>(b, static_cast<long long>(a.total_q) * a.n_heads, 0, 64, st)));
-    return hipSuccess;
+    const long long small_joins = small && p.small_chunks > 1 ? static_cast<long long>(heads) * a.n * p.small_rows : 0;
+    const long long joins = small_joins + (many && p.many_chunks > 1 ? static_cast<long long>(a.total_q) * a.n_heads : 0);
+    if (joins == 0) return hipSuccess;
+    const bool wide = (small_joins ? p.small_chunks : 0) > 8 || (joins > small_joins && p.many_chunks > 8);
+    const auto f = wide ? kv_combine_kernel<D, kWaves> : kv_combine_kernel<D, 1>;
+    const unsigned grid = static_cast<unsigned>(wide ? joins : (joins + kWaves - 1) / kWaves);
+    return launch_kernel(f, dim3(grid), dim3(kThreads), 0, st, a, m, small_joins, 16 * p.small_nb);
 }
 
 long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
 }  // namespace
 
-// Chunks. A work-group needs about 4.5 us whatever its keys and 0.7 us for each 128, and joining costs 4 us, so up to
-// 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001 tokens and 8
-// kv heads: chunks of 512 / 1,024 / 2,048 keys 16.9 / 15.4 / 19.0 us), and at least three to a request that is as long as
-// max_kv, because the others are shorter (64 requests of up to 3,872 tokens: one chunk 25.3, chunks of 1,024 23.5), but
-// not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 / 206).
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads) {
+// Short requests: chunks. A work-group needs about 4.5 us whatever its keys and 0.5 us for each 128, and joining costs 4
+// us, so up to 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001
+// tokens and 8 kv heads: chunks of 512 / 1,024 / 2,048 keys 16.9 / 15.4 / 19.0 us), and at least three to a request that is
+// as long as max_kv, because the others are shorter (64 requests of up to 3,872 tokens: one chunk 25.3, chunks of 1,024
+// 23.5), but not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 /
+// 206). Long requests: tiles of 64 rows where they fill the machine twice (2,048 tokens of 32 heads over 16,000 keys: 483 us,
+// tiles of 32 rows 536), else of 32, of which a CU runs three and whose steps take 0.75 us for 1.6 (2 x 185 tokens of 20
+// heads over 2,676 keys 42 and 26 us); where their rows are more than 1,024, joining costs more, and only half a fill is split.
+KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int window) {
     KvAttnPlan p{};
     const int group = n_heads / n_kv_heads;
     const long long most = static_cast<long long>(max_q) * group;
-    auto split = [&](long long work_groups, int least, int* chunk, int* chunks) {
-        long long c = max_kv;
-        if (max_kv > 1024) {
-            long long want = (256 + work_groups - 1) / work_groups;
-            want = want < least ? least : want;
-            if (want > 1) {
-                c = round_up((max_kv + want - 1) / want, 128);
-                c = c < 256 ? 256 : c > 2048 && least > 1 ? 2048 : c;
-            }
+    // keys that a tile (at most 64 tokens) can see, on whole records
+    const long long reach = window > 0 && window < max_kv ? static_cast<long long>(window) + (max_q < 64 ? max_q : 64) + kRecTokens : max_kv;
+    const long long keys = reach < max_kv ? reach : max_kv;
+    // Chunks of the keys, about `want`; returns how many there can be for these sizes with any window: the workspace
+    // does not depend on it.
+    auto split = [&](long long want, long long least, long long largest, int* chunk, int* chunks) {
+        long long c = keys;
+        if (keys > 1024 && want > 1) {
+            c = round_up((keys + want - 1) / want, 128);
+            c = c < least ? least : c > largest ? largest : c;
         }
         *chunk = static_cast<int>(c < 1 ? 1 : round_up(c, 16));
-        *chunks = max_kv > *chunk ? (max_kv + *chunk - 1) / *chunk : 1;
+        *chunks = static_cast<int>(keys > *chunk ? (keys + *chunk - 1) / *chunk : 1);
+        if (max_kv <= 1024 || want <= 1) return 1LL;
+        const long long by_size = (max_kv + largest - 1) / largest;
+        return want > by_size ? want : by_size;
     };
-    // one tile of 16, 32 or 64 rows holds a request, or (of longer ones) at least a single token
-    const long long fit = most <= 64 ? most : group;
-    if (fit <= 64) {
-        p.small_nb = fit <= 16 ? 1 : fit <= 32 ? 2 : 4;
+    long long small_most = 1, many_most = 1;
+    // one tile of 16 or 32 rows holds a request, or (of longer ones) at least a single token
+    const long long fit = most <= 32 ? most : group;
+    if (fit <= 32) {
+        p.small_nb = fit <= 16 ? 1 : 2;
         p.small = 16 * p.small_nb;
         p.small_rows = static_cast<int>(most < p.small ? most : p.small);
         p.many = most > p.small;
         if (p.many && static_cast<long long>(n) * max_q == total_q) p.small_rows = 0;  // every request is long
-        split(static_cast<long long>(n) * n_kv_heads, 3, &p.small_chunk, &p.small_chunks);
+        const long long per = static_cast<long long>(n) * n_kv_heads, want = (256 + per - 1) / per;
+        small_most = split(want < 3 ? 3 : want, 256, 2048, &p.small_chunk, &p.small_chunks);
     } else {
         p.many = true;
     }
     p.many_chunks = 1;
     if (p.many) {
         const long long rows = static_cast<long long>(total_q) * group, longer = rows / (p.small + 1);
-        p.many_tiles = static_cast<int>(rows / 64 + (longer < n ? longer : n));  // at most: every long request's last tile cut
-        split((rows / 64 + 1) * n_kv_heads, 1, &p.many_chunk, &p.many_chunks);
+        p.many_nb = (rows / 64 + 1) * n_kv_heads < 1024 ? 2 : 4;
+        const int tile = 16 * p.many_nb;
+        p.many_tiles = static_cast<int>(rows / tile + (longer < n ? longer : n));  // at most: every long request's last tile cut
+        const long long per = (rows / tile + 1) * n_kv_heads;
+        const long long fill = rows <= 1024 ? 256 : 128;
+        many_most = split((fill + per - 1) / per, rows <= 1024 ? 512 : 1024, max_kv, &p.many_chunk, &p.many_chunks);
     }
-    p.small_parts = p.small_rows > 0 && p.small_chunks > 1 ? static_cast<size_t>(n) * n_kv_heads * p.small_rows * p.small_chunks : 0;
-    p.many_parts = p.many && p.many_chunks > 1 ? static_cast<size_t>(total_q) * n_heads * p.many_chunks : 0;
+    p.small_parts = p.small_rows > 0 && small_most > 1 ? static_cast<size_t>(n) * n_kv_heads * p.small_rows * small_most : 0;
+    p.many_parts = p.many && many_most > 1 ? static_cast<size_t>(total_q) * n_heads * many_most : 0;
+    p.small_most = small_most;
+    p.many_most = many_most;
     return p;
+}
+
+// At most, with any window, work-groups of a launch.
+long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads) {
+    return n_kv_heads * (static_cast<long long>(n) * p.small_most + static_cast<long long>(p.many_tiles) * p.many_most);
 }
 
 hipError_t launch_kv_attention(KvAttnArgs a, const KvAttnPlan& p, hipStream_t st) {

@@ -22,7 +22,8 @@ constexpr int kThreads = 512;
 constexpr int kChunk = 4096;          // tokens of a work-group
 constexpr int kVecs = kChunk / (4 * kThreads);  // groups of four a thread
 constexpr uint32_t kPrompt = 1u << 31;  // seen in the prompt
-constexpr uint32_t kBias = 1u << 30;    // has a bias; below it the count past the prompt
+constexpr uint32_t kBias = 1u << 30;    // has a bias
+constexpr uint32_t kAgain = 1u << 29;   // more than one; below it the count past the prompt
 
 template <bool BF16>
 __device__ __forceinline__ float load1(const void* p, long long i) {
@@ -122,41 +123,39 @@ __global__ __launch_bounds__(kThreads) void logits_adjust_kernel(LogitsArgs a) {
             }
         }
     }
-    // Biases: a wave looks at 64 entries; each of theirs that falls into the stretch and is the list's first of its token
-    // collects the others from the list, all lanes comparing.
-    const int lane = tid & (kWave - 1), wid = tid / kWave;
-    for (long long base = b0 + wid * kWave; base < b1; base += kThreads) {
-        const int mine = base + lane < b1 ? a.bias_tokens[base + lane] : -1;
-        uint64_t todo = __ballot(mine >= v0 && mine < v1);
-        while (todo) {
-            const int l = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const int v = __shfl(mine, l, kWave);
-            float sum = 0.f;
-            bool any = false, first = true;
-            for (long long c = b0; c < b1; c += kWave) {  // uniform
-                const bool in_list = c + lane < b1;
-                uint64_t same = __ballot(in_list && a.bias_tokens[in_list ? c + lane : c] == v);
-                if (!any && same && c + __builtin_ctzll(same) != base + l) first = false;
-                if (!first) break;
-                while (same) {
-                    const float b = a.bias_values[c + __builtin_ctzll(same)];
-                    same &= same - 1;
-                    sum = any ? sum + b : b;
-                    any = true;
-                }
+    // Biases. Entry i of the list, if it falls into the stretch, is alone with its token unless another entry leaves a
+    // smaller index in `bias` (as a number); then the token is marked. The entry that is alone puts its value there, and
+    // of a marked token's the list's first puts the sum, having looked through the list, in order.
+    if (b0 < b1) {
+        auto each = [&](auto&& f) {
+            for (long long i = b0 + tid; i < b1; i += kThreads) {
+                const int v = a.bias_tokens[i];
+                if (v >= v0 && v < v1) f(static_cast<int>(i - b0), v - body + 4);
             }
-            if (first && lane == 0) {
-                bias[v - body + 4] = sum;
-                atomicOr(&seen[v - body + 4], kBias);
+        };
+        int* first = reinterpret_cast<int*>(bias);
+        each([&](int, int at) { first[at] = INT32_MAX; });
+        __syncthreads();
+        each([&](int i, int at) { atomicMin(&first[at], i); });
+        __syncthreads();
+        each([&](int i, int at) { atomicOr(&seen[at], first[at] == i ? kBias : kAgain); });
+        __syncthreads();
+        each([&](int i, int at) {
+            float sum = a.bias_values[b0 + i];
+            if (seen[at] & kAgain) {
+                for (long long j = b0; j < b0 + i; ++j)
+                    if (a.bias_tokens[j] - body + 4 == at) return;
+                for (long long j = b0 + i + 1; j < b1; ++j)
+                    if (a.bias_tokens[j] - body + 4 == at) sum += a.bias_values[j];
             }
-        }
+            bias[at] = sum;
+        });
     }
     __syncthreads();
 
     auto adjust = [&](float z, uint32_t s, int at) {
-        if (s & ~kBias) z = z > 0.f ? z / rep : z * rep;
-        const uint32_t c = s & ~(kPrompt | kBias);
+        if (s & ~(kBias | kAgain)) z = z > 0.f ? z / rep : z * rep;
+        const uint32_t c = s & ~(kPrompt | kBias | kAgain);
         if (c) z = __fsub_rn(__fsub_rn(z, __fmul_rn(freq, static_cast<float>(c))), pres);
         if (s & kBias) z += bias[at];
         return z;
