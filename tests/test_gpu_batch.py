@@ -242,6 +242,42 @@ def test_attention(q_lens, kv_lens, heads, kv_heads, d, page, window):
     assert (host(wide_out)[T:] == 5).all() and (host(wide_out)[:, 0] == 5).all() and (host(wide_out)[:, 1 + heads * d:] == 5).all()
 
 
+@pytest.mark.parametrize("heads,kv_heads,d,window,q_lens,kv_lens", [
+    (128, 128, 64, 0, [300, 0, 250], [300, 7, 400]),           # tiles of 64 rows
+    (128, 128, 128, 90, [300, 1, 250, 1], [300, 700, 310, 30]),  # beside single tokens
+    (160, 8, 64, 0, [2, 1, 230, 1], [50, 70, 230, 1]),         # groups of 20: tiles of 32 for single tokens, beside them
+    (128, 128, 64, 0, [20], [4500]),                           # keys past what the lanes hold pages for
+    (128, 64, 64, 0, [450, 1, 12], [450, 900, 4200])])
+def test_attention_of_many_rows(heads, kv_heads, d, window, q_lens, kv_lens):
+    note(f"kv attention q={q_lens} kv={kv_lens} heads={heads}/{kv_heads} d={d} window={window}")
+    rng = np.random.default_rng(heads + d)
+    cache, blocks, k, v, _ = paged(rng, kv_lens, kv_heads, d, 16)
+    q = torch.from_numpy(rng.standard_normal((sum(q_lens), heads, d))).to("cuda").to(BF)
+    out = cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(blocks), max(q_lens), max(kv_lens), window=window)
+    assert cache.status() == (E.ELIS_OK, 0)
+    check_attention(out, q, q_lens, kv_lens, k, v, d ** -0.5, window)
+
+
+def test_cache_past_four_gib():
+    """Records whose places pass 32 bits: append, read and attention on the last pages of a large cache."""
+    rng = np.random.default_rng(4)
+    d, heads, page, kv = 128, 16, 64, 150
+    n_pages = 5 * 2 ** 30 // (heads * page // 16 * 17 * d) + 1
+    note(f"kv cache of {n_pages} pages, {E.elis_kv_cache_bytes(n_pages, page, heads, d) / 2 ** 30:.1f} GiB")
+    cache = KVCache(n_pages, page, heads, d)
+    blocks = np.array([[n_pages - 1, 3, n_pages - 2]])
+    slots = i32(blocks[0, np.arange(kv) // page] * page + np.arange(kv) % page)
+    k, v = (torch.from_numpy(rng.standard_normal((kv, heads, d))).to("cuda").to(BF) for _ in range(2))
+    cache.append(k, v, slots)
+    rk, rv = torch.empty_like(k), torch.empty_like(v)
+    cache.read(slots, rk, rv)
+    assert np.array_equal(host(rk)[[0, 70, 149]], O.kv_round(host(k)[[0, 70, 149]])) and np.array_equal(host(rv)[[63, 64]], O.kv_round(host(v)[[63, 64]]))
+    for n in (1, 40):
+        q = torch.from_numpy(rng.standard_normal((n, heads, d))).to("cuda").to(BF)
+        out = cache.attention(q, i32([0, n]), i32([kv]), i32(blocks), n, kv)
+        check_attention(out, q, [n], [kv], host(rk), host(rv), d ** -0.5)
+
+
 @pytest.mark.parametrize("q_len", [1, 40, 300])
 def test_attention_masked_pages_and_nan(q_len):
     """Keys on bad pages are not seen; NaN in a key or a value reaches the rows that see it, and no other."""
@@ -375,6 +411,38 @@ def test_logits(n, vocab, hist, pad, dtype):
         adjust_logits(x, i32(ids), i32(cu), out=full[:n, 3:], **kw)
         adjust_logits(y, i32(ids), i32(cu), out=y, **kw)
         assert torch.equal(y, full[:n, 3:])
+
+
+def test_logits_of_crowded_rows():
+    """One token over and over, as many biases as tokens and every one twice, prompts as long as the history, no mask bit set."""
+    rng = np.random.default_rng(8)
+    n, vocab = 3, 5000
+    x = torch.from_numpy(rng.standard_normal((n, vocab)).astype(np.float32)).cuda()
+    ids = np.concatenate([np.full(20000, 4321), rng.integers(0, vocab, 3000), [7]])
+    cu = np.array([0, 20000, 23000, 23001])
+    tok = np.concatenate([rng.permutation(vocab)] * 2)
+    val = rng.standard_normal(len(tok)).astype(np.float32)
+    note("logits: crowded rows")
+    out = adjust_logits(x, i32(ids), i32(cu), prompt_lens=i32([5, 3000, 9]), frequency=dev(np.full(n, 0.01, np.float32)),
+                        presence=dev(np.full(n, 0.5, np.float32)), repetition=dev(np.full(n, 2.0, np.float32)),
+                        bias=(i32([0, 2 * vocab, 2 * vocab, 2 * vocab]), i32(tok), dev(val)),
+                        mask=dev(np.zeros((1, 157), np.int32)), mask_rows=i32([-1, -1, 0]))
+    total = np.zeros(vocab)
+    np.add.at(total, tok, val.astype(np.float64))
+    for i, (h, p) in enumerate(((ids[:20000], 5), (ids[20000:23000], 3000), (ids[23000:], 9))):
+        f = float(np.float32(0.01))
+        y = O.logits_adjust(host(x)[i], h.tolist()[:p] + h.tolist()[p:p + 1], p, 2.0, f, 0.5, [], None)
+        count = max(0, len(h) - p)
+        if i == 0:
+            y[4321] -= f * (count - 1)       # the oracle has seen it once
+            y += total
+        if i == 2:
+            y[:] = -np.inf
+        got = host(out)[i]
+        assert np.array_equal(np.isneginf(got), np.isneginf(y))
+        size = np.abs(host(x)[i]) * 2 + f * count + 0.5 + (np.abs(val).max() * 2 if i == 0 else 0)
+        fin = np.isfinite(y)
+        assert (np.abs(got[fin] - y[fin]) <= 7 * 2.0 ** -24 * size[fin]).all()
 
 
 # ------------------------------------------------------------------ together
