@@ -5,8 +5,8 @@
 // all in fp32. The logits are read once and written once; everything else is small beside them. A work-group takes a
 // row's stretch of kChunk tokens: it requests the stretch's logits, counts the history's tokens that fall into it in LDS
 // (every work-group of a row reads the whole history, which the L2 holds), sums the row's biases of its tokens into LDS,
-// and then makes one pass over the registers. Of a token that a bias list names more than once the first entry sums them
-// all, in list order, so the result does not depend on timing; the counters are integers, whose atomics commute.
+// and then makes one pass over the registers. Biases of one token are added up in list order, so the result does not
+// depend on timing; the counters are integers, whose atomics commute.
 #include <math.h>
 
 #include "kernels.h"
@@ -22,8 +22,8 @@ constexpr int kThreads = 512;
 constexpr int kChunk = 4096;          // tokens of a work-group
 constexpr int kVecs = kChunk / (4 * kThreads);  // groups of four a thread
 constexpr uint32_t kPrompt = 1u << 31;  // seen in the prompt
-constexpr uint32_t kBias = 1u << 30;    // has a bias
-constexpr uint32_t kAgain = 1u << 29;   // more than one; below it the count past the prompt
+constexpr uint32_t kBias = 1u << 30;    // has a bias; below it the count past the prompt
+constexpr int kTurns = 1024;            // places at which the entries of a bias list take turns
 
 template <bool BF16>
 __device__ __forceinline__ float load1(const void* p, long long i) {
@@ -45,6 +45,7 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void logits_adjust_kernel(LogitsArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t seen[kChunk + 4];
     __shared__ float bias[kChunk + 4];  // of the tokens whose counter has kBias
+    __shared__ int turn[kTurns];
     const int row = blockIdx.y, tid = threadIdx.x;
     float* out = a.out + static_cast<long long>(row) * a.out_stride;
     const void* in = BF16 ? static_cast<const void*>(static_cast<const uint16_t*>(a.logits) + static_cast<long long>(row) * a.in_stride)
@@ -123,39 +124,38 @@ __global__ __launch_bounds__(kThreads) void logits_adjust_kernel(LogitsArgs a) {
             }
         }
     }
-    // Biases. Entry i of the list, if it falls into the stretch, is alone with its token unless another entry leaves a
-    // smaller index in `bias` (as a number); then the token is marked. The entry that is alone puts its value there, and
-    // of a marked token's the list's first puts the sum, having looked through the list, in order.
+    // Biases, an entry a thread and kThreads of the list at a time. Entries whose tokens share a place of `turn` (those of
+    // one token do) go one after the other in list order; nearly always there is one turn. A work-group none of whose
+    // tokens the entries name passes one barrier.
     if (b0 < b1) {
-        auto each = [&](auto&& f) {
-            for (long long i = b0 + tid; i < b1; i += kThreads) {
-                const int v = a.bias_tokens[i];
-                if (v >= v0 && v < v1) f(static_cast<int>(i - b0), v - body + 4);
+        for (int i = tid; i < kTurns; i += kThreads) turn[i] = kThreads;
+        for (long long base = b0; base < b1; base += kThreads) {
+            const long long i = base + tid;
+            const int v = i < b1 ? a.bias_tokens[i] : -1;
+            bool waits = v >= v0 && v < v1;
+            const int at = v - body + 4;
+            const float add = waits ? a.bias_values[i] : 0.f;
+            while (__syncthreads_or(waits)) {
+                int* place = &turn[at & (kTurns - 1)];
+                if (waits) atomicMin(place, tid);
+                __syncthreads();
+                const bool mine = waits && *place == tid;
+                if (mine) {
+                    const uint32_t s = seen[at];
+                    bias[at] = s & kBias ? bias[at] + add : add;
+                    seen[at] = s | kBias;
+                    waits = false;
+                }
+                __syncthreads();
+                if (mine) *place = kThreads;
             }
-        };
-        int* first = reinterpret_cast<int*>(bias);
-        each([&](int, int at) { first[at] = INT32_MAX; });
-        __syncthreads();
-        each([&](int i, int at) { atomicMin(&first[at], i); });
-        __syncthreads();
-        each([&](int i, int at) { atomicOr(&seen[at], first[at] == i ? kBias : kAgain); });
-        __syncthreads();
-        each([&](int i, int at) {
-            float sum = a.bias_values[b0 + i];
-            if (seen[at] & kAgain) {
-                for (long long j = b0; j < b0 + i; ++j)
-                    if (a.bias_tokens[j] - body + 4 == at) return;
-                for (long long j = b0 + i + 1; j < b1; ++j)
-                    if (a.bias_tokens[j] - body + 4 == at) sum += a.bias_values[j];
-            }
-            bias[at] = sum;
-        });
+        }
     }
     __syncthreads();
 
     auto adjust = [&](float z, uint32_t s, int at) {
-        if (s & ~(kBias | kAgain)) z = z > 0.f ? z / rep : z * rep;
-        const uint32_t c = s & ~(kPrompt | kBias | kAgain);
+        if (s & ~kBias) z = z > 0.f ? z / rep : z * rep;
+        const uint32_t c = s & ~(kPrompt | kBias);
         if (c) z = __fsub_rn(__fsub_rn(z, __fmul_rn(freq, static_cast<float>(c))), pres);
         if (s & kBias) z += bias[at];
         return z;
