@@ -477,15 +477,16 @@ int elis_kv_init(const elis_kv_cache *c, void *stream);
 
 /*
  * Keys and values of n_tokens new tokens into the slots of slot_map (device
- * int32 [n_tokens]; -1: the token is not kept). k, v: bf16, token t's row at t *
+ * int32 [n_tokens]; -1: the token is not kept; neither is it at any other slot
+ * outside the cache, with ELIS_DEV_BAD_PAGE). k, v: bf16, token t's row at t *
  * stride elements, head h at h * d_head in it (rows may be part of a wider
  * matrix: strides of at least n_kv_heads * d_head). 16-byte aligned rows load
- * widest; others are served too. No slot may be named twice.
+ * widest; others are served too. What a slot named twice holds is undefined.
  */
 int elis_kv_append(const elis_kv_cache *c, const uint16_t *k, const uint16_t *v, int64_t k_stride, int64_t v_stride,
                    const int32_t *slot_map, int32_t n_tokens, void *stream);
 
-/* What the cache keeps of the tokens in slot_map, as bf16 (exact; zeros for slot -1). Layout as elis_kv_append. */
+/* What the cache keeps of the tokens in slot_map, as bf16 (exact; zeros where there is none). Layout as elis_kv_append. */
 int elis_kv_read(const elis_kv_cache *c, const int32_t *slot_map, int32_t n_tokens, uint16_t *out_k, uint16_t *out_v,
                  int64_t k_stride, int64_t v_stride, void *stream);
 
@@ -506,7 +507,7 @@ size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max
  *  blocks      int32 [block_rows, blocks_stride]: page ids in token order; request i's row is
  *              rows[i] (device int32 [n]; with a pool's table and slots no copy is needed), or i if rows is NULL.
  *              A key on an id outside the cache is not seen (ELIS_DEV_BAD_PAGE).
- *  kv_lens     int32 [n].   scale > 0.
+ *  kv_lens     int32 [n].   scale > 0 (times log2(e) still finite).
  *  workspace   256-byte aligned, elis_kv_attention_workspace_bytes() bytes.
  * Products of bf16 operands (the keys and values are exact in bf16, the weights
  * are rounded once) with fp32 sums and statistics. n <= 65535; max_kv <=
@@ -534,7 +535,7 @@ int elis_kv_attention(const elis_kv_cache *c, const uint16_t *q, int64_t q_strid
  * fp32 and the strides are equal).
  *  logits       ELIS_DT_F32 or ELIS_DT_BF16 [n, vocab], row i at i * in_stride elements; out at i * out_stride.
  *  token_ids    int32 [total_tokens] or NULL (no history; then cu_seqlens and prompt_lens are not read).
- *               Ids outside [0, vocab) are passed over; ranges are cut to [0, total_tokens).
+ *               Ids outside [0, vocab) are passed over; ranges are cut to [0, total_tokens). At most 2^29.
  *  prompt_lens  int32 [n] or NULL (no prompts: everything counts).
  *  repetition, frequency, presence   fp32 [n] each, or NULL (1, 0, 0).
  *  bias_cu      int32 [n + 1] or NULL: row i's biases are bias_tokens / bias_values[bias_cu[i] .. bias_cu[i+1]-1]

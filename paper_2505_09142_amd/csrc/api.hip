@@ -835,13 +835,15 @@ int elis_kv_attention(const elis_kv_cache* c, const uint16_t* q, int64_t q_strid
                       int32_t window, uint16_t* out, int64_t out_stride, void* workspace, size_t ws_bytes, void* stream) {
     int r = check_cache(c);
     if (r != ELIS_OK) return r;
-    if (!q || !cu_q || !blocks || !kv_lens || !out || !workspace || !aligned(workspace)) return ELIS_EINVAL;
-    if (!(scale > 0.f) || !isfinite(scale) || window < 0 || block_rows < 1 || blocks_stride < 1) return ELIS_EINVAL;
+    if ((total_q != 0 && (!q || !out)) || !cu_q || !blocks || !kv_lens || !workspace || !aligned(workspace)) return ELIS_EINVAL;
+    const float scale_log2 = scale * 1.44269504088896340736f;
+    if (!(scale > 0.f) || !isfinite(scale_log2) || window < 0 || block_rows < 1 || blocks_stride < 1) return ELIS_EINVAL;
     r = check_kv_attention_sizes(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads, c->d_head);
     if (r != ELIS_OK) return r;
     const int64_t row = static_cast<int64_t>(n_heads) * c->d_head;
     if (q_stride < row || out_stride < row || static_cast<int64_t>(blocks_stride) * c->page_tokens < max_kv || (!rows && block_rows < n))
         return ELIS_ESHAPE;
+    if (window >= max_kv) window = 0;  // every key before a token is in it (and positions less a window stay in range)
     const KvAttnPlan p = plan_kv_attention(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads, window);
     if (ws_bytes < kv_attention_ws(p, c->d_head)) return ELIS_EWORKSPACE;
     if (total_q == 0) return ELIS_OK;
@@ -863,7 +865,7 @@ int elis_kv_attention(const elis_kv_cache* c, const uint16_t* q, int64_t q_strid
     a.max_kv = max_kv;
     a.n_heads = n_heads;
     a.group = n_heads / c->n_kv_heads;
-    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.scale_log2 = scale_log2;
     a.window = window;
     a.out = out;
     a.out_stride = out_stride;
@@ -884,7 +886,7 @@ int elis_logits_adjust(const void* logits, int32_t dtype, int64_t in_stride, int
     if (!logits || !out || (token_ids && !cu_seqlens) || (bias_cu && bias_total > 0 && (!bias_tokens || !bias_values))) return ELIS_EINVAL;
     if (mask && n_masks < 1) return ELIS_EINVAL;
     if (in_stride < vocab || out_stride < vocab || (mask && mask_stride < (static_cast<int64_t>(vocab) + 31) / 32)) return ELIS_ESHAPE;
-    if (n > 65535 || vocab > (1 << 28)) return ELIS_ESHAPE;
+    if (n > 65535 || vocab > (1 << 28) || total_tokens > (1 << 29)) return ELIS_ESHAPE;
     if (logits == out && (dtype != ELIS_DT_F32 || in_stride != out_stride)) return ELIS_EINVAL;
     if (mask && !mask_rows && n_masks < n) return ELIS_ESHAPE;
     LogitsArgs a{};

@@ -3,7 +3,9 @@
 // Rows. The queries of one request that read the same kv head (its new tokens times the n_heads / n_kv_heads query
 // heads of the group) are the rows of one product: row r is token r / G, head r % G of the group. A work-group takes 16
 // NB rows of a (request, kv head) and one chunk of the keys they see; its four waves split the chunk's keys and each
-// streams its own records straight from memory into registers, so nothing but the final merge passes through LDS.
+// streams its own records straight from memory into registers, so nothing but the query rows (NB 2 and 4: their registers
+// are what another wave on the SIMD needs) and the final merge passes through LDS. NB is 1 or 2 for requests of up to 16
+// or 32 rows, single tokens above all, and 2 or 4 for tiles of longer ones.
 //
 // Products. As the encoder's attention: S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_16x16x32_bf16, the accumulators of
 // the first being, rounded to bf16, the P^T operand of the second (lane group g holds keys 4g..4g+3 of each of a step's
@@ -22,9 +24,13 @@
 // zeroed, so what lies there cannot matter; a group of values that holds NaN (scale 255) is multiplied as zero and
 // makes NaN of exactly the rows that see it (where every row sees a record, its NaN goes through the products).
 //
-// Bound by memory for single tokens: 17/16 D bytes a key and kv head, once. The vector unit comes second: about 180
-// instructions a 32-key step of a wave. Few rows are split over the keys (chunks) and joined by a second launch.
+// Bounds. Single tokens: memory, 17/16 D bytes a key and kv head, once (48 requests of 16,000 tokens and 8 kv heads of 128:
+// 207 us, 5.0 TB/s, more than a copy reaches). Long prompts: the vector unit, which unpacks and takes exponentials beside
+// the products (2,048 tokens of 32 heads over 16,000 keys: 484 us, 1.04 PFLOP/s; vector unit busy 65 % of it, matrix unit
+// 41 %). One request alone: latency. Its keys are split (chunks) and joined by a second launch.
 #include <math.h>
+
+#include <type_traits>
 
 #include "kv_cache.h"
 
@@ -58,6 +64,16 @@ __device__ __forceinline__ float dot2(uint32_t w, float s) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), s, false);
 #else
     return s;
+#endif
+}
+
+// Byte S of w, two E2M1 values times a power of two, as a pair of bf16 (exact).
+template <int S>
+__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, S));
+#else
+    return 0u;
 #endif
 }
 
@@ -347,184 +363,182 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
         }
         const int w0 = span + wid * kStep, w1 = span + kSpan < k1 ? span + kSpan : k1;
         const int steps = w0 < w1 ? (w1 - w0 + kWaves * kStep - 1) / (kWaves * kStep) : 0;
-    for (int st = 0; st < steps; ++st) {
-        // keeps the query rows in LDS: reads of memory that does not change would be moved out of the loop, into registers
-        if constexpr (QLDS) asm volatile("" ::: "memory");
-        Step next;
-        if constexpr (!INPLACE) load(st + 1, next);
-        const int kb = w0 + st * (kWaves * kStep);
-        bool there[2];
+        for (int st = 0; st < steps; ++st) {
+            // keeps the query rows in LDS: reads of memory that does not change would be moved out of the loop, into registers
+            if constexpr (QLDS) asm volatile("" ::: "memory");
+            Step next;
+            if constexpr (!INPLACE) load(st + 1, next);
+            const int kb = w0 + st * (kWaves * kStep);
+            bool there[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) there[u] = __builtin_amdgcn_readlane(off_hi, (2 * st + u) & 63) >= 0;
-        // Uniform: some key of the step is not seen by some row.
-        const bool edge = kb + kStep > all_hi || kb < all_lo || !there[0] || !there[1];
-        uint32_t pw[NB][4];  // the weights, as the second product's operand
-        // Of two waves on a SIMD the one that multiplies goes first: the other's exponentials fill in behind (498 -> 466 us
-        // for 2,048 tokens over 16,000).
-        if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
+            for (int u = 0; u < 2; ++u) there[u] = __builtin_amdgcn_readlane(off_hi, (2 * st + u) & 63) >= 0;
+            // Uniform: some key of the step is not seen by some row.
+            const bool edge = kb + kStep > all_hi || kb < all_lo || !there[0] || !there[1];
+            uint32_t pw[NB][4];  // the weights, as the second product's operand
+            // Of two waves on a SIMD the one that multiplies goes first: the other's exponentials fill in behind (498 -> 466 us
+            // for 2,048 tokens over 16,000).
+            if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int u0 = 0; u0 < 2; u0 += UB) {
-            f32x4 s[UB][NB];
+            for (int u0 = 0; u0 < 2; u0 += UB) {
+                f32x4 s[UB][NB];
 #pragma unroll
-            for (int u = 0; u < UB; ++u)
+                for (int u = 0; u < UB; ++u)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) s[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int j = 0; j < NB; ++j) s[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                bf16x8 q[NB];
+                for (int t = 0; t < KS; ++t) {
+                    bf16x8 q[NB];
 #pragma unroll
-                for (int j = 0; j < NB; ++j) q[j] = query(j, t);
+                    for (int j = 0; j < NB; ++j) q[j] = query(j, t);
 #pragma unroll
-                for (int u = 0; u < UB; ++u) {
-                    const uint32_t w = x.k[u0 + u][t];
-                    const float ksc = __uint_as_float(x.ks[u0 + u] << 23);
-                    const u32x4 kk = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 0)),
-                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 1)),
-                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 2)),
-                                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, ksc, 3))};
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), q[j], s[u][j], 0, 0, 0);
-                }
-            }
-            if constexpr (INPLACE) __builtin_amdgcn_s_setprio(0);
-            if (edge) {
-                int from[NB];        // row c of block j sees the keys from, from + 1, ..., from + more; none: from lies past all
-                uint32_t more[NB];
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const int pos = back + token(j), f = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-                    from[j] = pos < 0 ? INT32_MAX : f;
-                    more[j] = pos < 0 ? 0u : static_cast<uint32_t>(pos - f);
-                }
-#pragma unroll
-                for (int u = 0; u < UB; ++u) {
-                    const int v = u0 + u, kv = there[v] ? kb + 16 * v : INT32_MIN;  // a record that is not there: before all keys
-                    uint32_t nan = 0u;  // of this lane's four keys, those whose values are NaN
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = kv + 4 * g + i;
+                    for (int u = 0; u < UB; ++u) {
+                        const uint32_t w = x.k[u0 + u][t];
+                        const float ksc = __uint_as_float(x.ks[u0 + u] << 23);
+                        const u32x4 kk = {two_values<0>(w, ksc), two_values<1>(w, ksc), two_values<2>(w, ksc), two_values<3>(w, ksc)};
 #pragma unroll
                         for (int j = 0; j < NB; ++j)
-                            if (static_cast<uint32_t>(key) - static_cast<uint32_t>(from[j]) > more[j]) s[u][j][i] = -INFINITY;
-                        // values that no row may see, or that are NaN, multiply as zero
-                        const bool is_nan = ((x.vs[v] >> (8 * i)) & 0xFFu) == 0xFFu;
-                        if (is_nan) {
-                            x.vs[v] ^= 0xFFu << (8 * i);
-                            nan |= key < hi ? 1u << i : 0u;
-                        }
-                        if (is_nan || key >= hi) {
-                            if constexpr (D == 128) x.v[v][i] = 0u;
-                            else x.v[v][i >> 1] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;
-                        }
+                            s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), q[j], s[u][j], 0, 0, 0);
                     }
-                    if (__ballot(nan != 0u) != 0ull) {
-                        // lane (c, g) of O^T holds columns 4g..4g+3: values D/4 g ..., of the scale group that lane
-                        // (from_c, g') read for the keys 4g'..4g'+3
-                        const int from_c = g * (D / 4) / 32 * (32 / DB);
-#pragma unroll 1
-                        for (int y = 0; y < 16; ++y) {
-                            const uint32_t w = __shfl(nan, (y >> 2) * 16 + from_c, kWave);
+                }
+                if constexpr (INPLACE) __builtin_amdgcn_s_setprio(0);
+                if (edge) {
+                    int from[NB];        // row c of block j sees the keys from, from + 1, ..., from + more; none: from lies past all
+                    uint32_t more[NB];
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const int pos = back + token(j), f = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+                        from[j] = pos < 0 ? INT32_MAX : f;
+                        more[j] = pos < 0 ? 0u : static_cast<uint32_t>(pos - f);
+                    }
+#pragma unroll
+                    for (int u = 0; u < UB; ++u) {
+                        const int v = u0 + u, kv = there[v] ? kb + 16 * v : INT32_MIN;  // a record that is not there: before all keys
+                        uint32_t nan = 0u;  // of this lane's four keys, those whose values are NaN
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = kv + 4 * g + i;
 #pragma unroll
                             for (int j = 0; j < NB; ++j)
-                                if (((w >> (y & 3)) & 1u) && static_cast<uint32_t>(kv + y) - static_cast<uint32_t>(from[j]) <= more[j]) {
+                                if (static_cast<uint32_t>(key) - static_cast<uint32_t>(from[j]) > more[j]) s[u][j][i] = -INFINITY;
+                            // values that no row may see, or that are NaN, multiply as zero
+                            const bool is_nan = ((x.vs[v] >> (8 * i)) & 0xFFu) == 0xFFu;
+                            if (is_nan) {
+                                x.vs[v] ^= 0xFFu << (8 * i);
+                                nan |= key < hi ? 1u << i : 0u;
+                            }
+                            if (is_nan || key >= hi) {
+                                if constexpr (D == 128) x.v[v][i] = 0u;
+                                else x.v[v][i >> 1] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                            }
+                        }
+                        if (__ballot(nan != 0u) != 0ull) {
+                            // lane (c, g) of O^T holds columns 4g..4g+3: values D/4 g ..., of the scale group that lane
+                            // (from_c, g') read for the keys 4g'..4g'+3
+                            const int from_c = g * (D / 4) / 32 * (32 / DB);
+#pragma unroll 1
+                            for (int y = 0; y < 16; ++y) {
+                                const uint32_t w = __shfl(nan, (y >> 2) * 16 + from_c, kWave);
 #pragma unroll
-                                    for (int b = 0; b < DB; ++b) o[b][j] = f32x4{NAN, NAN, NAN, NAN};
-                                }
+                                for (int j = 0; j < NB; ++j)
+                                    if (((w >> (y & 3)) & 1u) && static_cast<uint32_t>(kv + y) - static_cast<uint32_t>(from[j]) <= more[j]) {
+#pragma unroll
+                                        for (int b = 0; b < DB; ++b) o[b][j] = f32x4{NAN, NAN, NAN, NAN};
+                                    }
+                            }
                         }
                     }
                 }
-            }
-            if constexpr (INPLACE) load_k(record(2 * st + 2 + u0), x, u0);
-            // The lanes of a row agree on m; whether to raise it each can tell from its own scores.
-            float t[NB], over = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                t[j] = max2(max3(s[0][j][0], s[0][j][1], s[0][j][2]), s[0][j][3]);
-                if constexpr (UB == 2) t[j] = max3(t[j], max3(s[1][j][0], s[1][j][1], s[1][j][2]), s[1][j][3]);
-            }
-#pragma unroll
-            for (int j = 0; j < NB; j += 2) {
-                const float x0 = fmaf(t[j], sc, -m[j]);
-                if (j + 1 < NB) over = max3(over, x0, fmaf(t[(j + 1) % NB], sc, -m[(j + 1) % NB]));
-                else over = x0;
-            }
-            if (__ballot(over > 8.f) != 0ull) {
+                if constexpr (INPLACE) load_k(record(2 * st + 2 + u0), x, u0);
+                // The lanes of a row agree on m; whether to raise it each can tell from its own scores.
+                float t[NB], over = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    const float mn = max2(m[j], ceilf(quad_max(t[j]) * sc));
-                    const float w = __builtin_amdgcn_exp2f(m[j] - mn);
-                    m[j] = mn;
-                    lsum[j] *= w;
+                    t[j] = max2(max3(s[0][j][0], s[0][j][1], s[0][j][2]), s[0][j][3]);
+                    if constexpr (UB == 2) t[j] = max3(t[j], max3(s[1][j][0], s[1][j][1], s[1][j][2]), s[1][j][3]);
+                }
 #pragma unroll
-                    for (int b = 0; b < DB; ++b)
+                for (int j = 0; j < NB; j += 2) {
+                    const float x0 = fmaf(t[j], sc, -m[j]);
+                    if (j + 1 < NB) over = max3(over, x0, fmaf(t[(j + 1) % NB], sc, -m[(j + 1) % NB]));
+                    else over = x0;
+                }
+                if (__ballot(over > 8.f) != 0ull) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[b][j][i] *= w;
-                    if (u0 > 0) {  // the first record's weights wait for the second product
+                    for (int j = 0; j < NB; ++j) {
+                        const float mn = max2(m[j], ceilf(quad_max(t[j]) * sc));
+                        const float w = __builtin_amdgcn_exp2f(m[j] - mn);
+                        m[j] = mn;
+                        lsum[j] *= w;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            pw[j][e] = pack_bf16x2(__uint_as_float(pw[j][e] << 16) * w, __uint_as_float(pw[j][e] & 0xFFFF0000u) * w);
+                        for (int b = 0; b < DB; ++b)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[b][j][i] *= w;
+                        if (u0 > 0) {  // the first record's weights wait for the second product
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                pw[j][e] = pack_bf16x2(__uint_as_float(pw[j][e] << 16) * w, __uint_as_float(pw[j][e] & 0xFFFF0000u) * w);
+                        }
                     }
                 }
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int u = 0; u < UB; ++u) {
+                        float p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][j][i], sc, -m[j]));
+                        const uint32_t w0 = pack_bf16x2(p[0], p[1]), w1 = pack_bf16x2(p[2], p[3]);
+                        pw[j][2 * (u0 + u)] = w0;
+                        pw[j][2 * (u0 + u) + 1] = w1;
+                        lsum[j] = dot2(w1, dot2(w0, lsum[j]));
+                    }
             }
+            bf16x8 pf[NB];
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j) pf[j] = __builtin_bit_cast(bf16x8, u32x4{pw[j][0], pw[j][1], pw[j][2], pw[j][3]});
+            if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
+            // V^T: for every pair of a column's values, the eight keys' pairs, then even and odd value as operands of two blocks
+            float vsc[8];
 #pragma unroll
-                for (int u = 0; u < UB; ++u) {
-                    float p[4];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][j][i], sc, -m[j]));
-                    const uint32_t w0 = pack_bf16x2(p[0], p[1]), w1 = pack_bf16x2(p[2], p[3]);
-                    pw[j][2 * (u0 + u)] = w0;
-                    pw[j][2 * (u0 + u) + 1] = w1;
-                    lsum[j] = dot2(w1, dot2(w0, lsum[j]));
+                for (int i = 0; i < 4; ++i) vsc[4 * u + i] = scale_of(x.vs[u], i);
+            auto pair = [&](auto sel) {
+                constexpr int S = decltype(sel)::value;
+                uint32_t y[8];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float s = vsc[4 * u + i];
+                        if constexpr (D == 128) y[4 * u + i] = two_values<S>(x.v[u][i], s);
+                        else y[4 * u + i] = i & 1 ? two_values<2 + (S & 1)>(x.v[u][i >> 1], s) : two_values<S & 1>(x.v[u][i >> 1], s);
+                    }
+                u32x4 ev, od;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ev[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x05040100u);
+                    od[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x07060302u);
                 }
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    o[2 * S][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ev), pf[j], o[2 * S][j], 0, 0, 0);
+                    o[2 * S + 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, od), pf[j], o[2 * S + 1][j], 0, 0, 0);
+                }
+            };
+            pair(std::integral_constant<int, 0>{});
+            pair(std::integral_constant<int, 1>{});
+            if constexpr (D == 128) {
+                pair(std::integral_constant<int, 2>{});
+                pair(std::integral_constant<int, 3>{});
+            }
+            if constexpr (INPLACE) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) load_v(record(2 * st + 2 + u), x, u);
+            } else {
+                x = next;
+            }
         }
-        bf16x8 pf[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) pf[j] = __builtin_bit_cast(bf16x8, u32x4{pw[j][0], pw[j][1], pw[j][2], pw[j][3]});
-        if constexpr (INPLACE) __builtin_amdgcn_s_setprio(1);
-        // V^T: for every pair of a column's values, the eight keys' pairs, then even and odd value as operands of two blocks
-        float vsc[8];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vsc[4 * u + i] = scale_of(x.vs[u], i);
-#define ELIS_VPAIR(SEL)                                                                                                                \
-    {                                                                                                                                  \
-        uint32_t y[8];                                                                                                                 \
-        _Pragma("unroll") for (int u = 0; u < 2; ++u) _Pragma("unroll") for (int i = 0; i < 4; ++i) {                                  \
-            if constexpr (D == 128)                                                                                                    \
-                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i], vsc[4 * u + i], SEL)); \
-            else if (i & 1)                                                                                                            \
-                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i >> 1], vsc[4 * u + i], 2 + ((SEL) & 1))); \
-            else                                                                                                                       \
-                y[4 * u + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[u][i >> 1], vsc[4 * u + i], (SEL) & 1)); \
-        }                                                                                                                              \
-        u32x4 ev, od;                                                                                                                  \
-        _Pragma("unroll") for (int e = 0; e < 4; ++e) {                                                                                \
-            ev[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x05040100u);                                                        \
-            od[e] = __builtin_amdgcn_perm(y[2 * e + 1], y[2 * e], 0x07060302u);                                                        \
-        }                                                                                                                              \
-        _Pragma("unroll") for (int j = 0; j < NB; ++j) {                                                                               \
-            o[2 * (SEL)][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ev), pf[j], o[2 * (SEL)][j], 0, 0, 0); \
-            o[2 * (SEL) + 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, od), pf[j], o[2 * (SEL) + 1][j], 0, 0, 0); \
-        }                                                                                                                              \
-    }
-        ELIS_VPAIR(0)
-        ELIS_VPAIR(1)
-        if constexpr (D == 128) {
-            ELIS_VPAIR(2)
-            ELIS_VPAIR(3)
-        }
-#undef ELIS_VPAIR
-        if constexpr (INPLACE) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) load_v(record(2 * st + 2 + u), x, u);
-        } else {
-            x = next;
-        }
-    }
     }
 
     // The four waves' parts, joined in wave order.
@@ -778,7 +792,7 @@ KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_he
         p.small = 16 * p.small_nb;
         p.small_rows = static_cast<int>(most < p.small ? most : p.small);
         p.many = most > p.small;
-        if (p.many && static_cast<long long>(n) * max_q == total_q) p.small_rows = 0;  // every request is long
+        if (p.many && static_cast<long long>(n) * max_q == total_q) p.small = p.small_rows = 0;  // every request looks long
         const long long per = static_cast<long long>(n) * n_kv_heads, want = (256 + per - 1) / per;
         small_most = split(want < 3 ? 3 : want, 256, 2048, &p.small_chunk, &p.small_chunks);
     } else {
@@ -801,9 +815,12 @@ KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_he
     return p;
 }
 
-// At most, with any window, work-groups of a launch.
+// At most, with any window, work-groups of a launch (or rows to join: a work-group each).
 long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads) {
-    return n_kv_heads * (static_cast<long long>(n) * p.small_most + static_cast<long long>(p.many_tiles) * p.many_most);
+    const long long small = static_cast<long long>(n) * n_kv_heads;
+    const long long parts = small * p.small_most + static_cast<long long>(n_kv_heads) * p.many_tiles * p.many_most;
+    const long long joins = p.small_most > 1 ? small * p.small_rows : 0;  // rows of long requests are fewer where they are split
+    return parts > joins ? parts : joins;
 }
 
 hipError_t launch_kv_attention(KvAttnArgs a, const KvAttnPlan& p, hipStream_t st) {

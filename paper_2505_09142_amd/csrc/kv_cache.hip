@@ -119,8 +119,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvCacheView c, cons
     if (t >= n) return;  // the four lanes of a scale have the same t
     const int at = map[t];
     const int page = at >> c.page_shift, pos = at & (c.page_tokens - 1), tok = pos & (kRecTokens - 1);
-    if (at < 0) return;  // a token without a slot
-    if (page >= c.n_pages) {
+    if (at == -1) return;  // a token without a slot
+    if (at < 0 || page >= c.n_pages) {
         if (h == 0 && sub == 0) atomicOr(c.status, ELIS_DEV_BAD_PAGE);
         return;
     }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCacheView c, const 
                  (static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(rec + R::val_at(tok, 2 * sub + 1))) << 16);
         xk = values_of(ck, rec[R::scale_k_at(tok, sub / 4)]);
         xv = values_of(cv, rec[R::scale_v_at(tok, sub / 4)]);
-    } else if (at >= 0 && h == 0 && sub == 0) {
+    } else if (at != -1 && h == 0 && sub == 0) {
         atomicOr(c.status, ELIS_DEV_BAD_PAGE);
     }
     store8<VEC>(k + t * k_stride + h * D + 8 * sub, xk);

@@ -6,6 +6,7 @@ kernels, reached through the same-named calls of ``_elis``.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import numpy as np
@@ -20,6 +21,10 @@ def _stream(stream) -> int:
     if stream is None:  # the handle itself: making torch's stream object costs as much as a launch (2.8 us)
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _torch_stream(stream) -> torch.cuda.Stream:
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
 
 
 def _to_dev(a: np.ndarray, device) -> torch.Tensor:
@@ -200,6 +205,12 @@ def _arg(t: torch.Tensor, dtype: torch.dtype, dev: int, where: str, at_least: in
     return t.data_ptr()
 
 
+def _made_on(dev: int, where: str):
+    """A state that a kernel of this call sets up has to lie on the current device."""
+    if dev < 0 or dev != _dev():
+        raise E.ElisError(E.ELIS_EINVAL, where)
+
+
 def _opt(t: torch.Tensor | None, dtype: torch.dtype, dev: int, where: str, at_least: int = 0) -> int | None:
     return None if t is None else _arg(t, dtype, dev, where, at_least)
 
@@ -243,6 +254,7 @@ class PagePool:
         self.p = E.elis_page_pool(*(t.data_ptr() for t in (*tensors, self.scratch)), n_pages, page_tokens, max_jobs,
                                   max_pages)
         if made:
+            _made_on(self.state.get_device(), "elis_pages_init")
             E.check(E.elis_pages_init(self.p, _stream(stream)), "elis_pages_init")
 
     def grow(self, slots: torch.Tensor, lens: torch.Tensor, cu_new: torch.Tensor | None, total_new: int,
@@ -289,8 +301,9 @@ class KVCache:
         self.buf, self.dev = buf, buf.get_device()
         self.c = E.elis_kv_cache(base, n_pages, page_tokens, n_kv_heads, d_head)
         self.ws = Workspace(buf.device)
-        self._sizes, self._ws = None, (0, 0)  # of the last attention call: its sizes, and the workspace they take
+        self._sizes, self._need = None, 0  # of the last attention call, and the workspace they take
         if made:
+            _made_on(self.dev, "elis_kv_init")
             E.check(E.elis_kv_init(self.c, _stream(stream)), "elis_kv_init")
 
     def _here(self, where: str) -> int:
@@ -333,9 +346,14 @@ class KVCache:
         block_rows, block_cols = blocks.shape
         sizes = (n, total, max_q, max_kv, heads)
         if sizes != self._sizes:
-            self._ws = self.ws.get(E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d))
-            self._sizes = sizes
-        ws, wsb = self._ws
+            self._need, self._sizes = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d), sizes
+        # A workspace of the call's own: calls on several streams, and captured graphs, share none but the one that holds
+        # nothing (256 bytes, not touched).
+        (ws, _), wsb = self.ws.get(256), self._need
+        if wsb > 256:
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream)):
+                scratch = torch.empty(wsb + 256, dtype=torch.uint8, device=q.device)
+            ws = (scratch.data_ptr() + 255) // 256 * 256
         E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, dev, where, n + 1), n, total, max_q,
                                     _arg(blocks, i32, dev, where), block_rows, block_cols,
                                     _opt(rows, i32, dev, where, n), _arg(kv_lens, i32, dev, where), max_kv, heads,

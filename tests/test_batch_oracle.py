@@ -128,3 +128,21 @@ def test_logits_refusals():
         assert call(**kw) == E.ELIS_EINVAL, kw
     for kw in (dict(xs=99), dict(os=99), dict(mask=FAKE, nm=2, ms=3), dict(mask=FAKE, nm=1, ms=4), dict(n=65536)):
         assert call(**kw) == E.ELIS_ESHAPE, kw
+    assert call(total=2 ** 29 + 1) == E.ELIS_ESHAPE
+
+
+def test_attention_of_nothing_and_scales_at_the_end():
+    c = E.elis_kv_cache(FAKE_WS, 64, 16, 2, 64)
+    call = lambda total, q, scale=0.1: E.elis_kv_attention(c, q, 256, FAKE, 2, total, 4, FAKE, 2, 8, None, FAKE, 100, 4, scale, 0, q, 256, FAKE_WS,  # noqa: E731
+                                                           1 << 20, None)
+    assert call(0, None) == E.ELIS_OK and call(1, None) == E.ELIS_EINVAL
+    assert call(0, FAKE, 2.0e38) == E.ELIS_OK and call(0, FAKE, 3.0e38) == E.ELIS_EINVAL  # times log2(e): past the range
+
+
+def test_state_off_the_device_is_refused():
+    """What a constructor would set up with a kernel has to lie on the current device."""
+    from paper_2505_09142_amd.device import KVCache, PagePool
+    with pytest.raises(E.ElisError):
+        PagePool(4, 16, 2, 2, device="cpu")
+    with pytest.raises(E.ElisError):
+        KVCache(4, 16, 2, 64, device="cpu")

@@ -93,6 +93,27 @@ def test_pages_content_errors():
     assert int(pool.state[1]) + int(pool.held.sum()) == 40
 
 
+@pytest.mark.parametrize("n,page,longest", [(100, 16, 9000), (5, 1024, 70000)])
+def test_pages_wide_tables_and_again(n, page, longest):
+    """Tables of many cells (two launches for few jobs); a call served again changes nothing; pages back by a trim."""
+    rng = np.random.default_rng(page)
+    W = -(-longest // page)
+    lens = rng.integers(1, longest + 1, n)
+    need = -(-lens // page)
+    pool, ref = PagePool(int(need.sum()), page, n, W), O.Pages(int(need.sum()), page, n, W)
+    slots, total = rng.permutation(n), int(lens.sum())
+    rb, rm = ref.grow(slots.tolist(), lens.tolist(), lens.tolist())
+    for turn in range(3):
+        note(f"pages wide n={n} page={page} turn={turn}")
+        blocks = torch.full((n, W), -9, dtype=torch.int32, device="cuda")
+        smap = torch.full((total,), -9, dtype=torch.int32, device="cuda")
+        pool.grow(i32(slots), i32(lens), i32(np.concatenate([[0], np.cumsum(lens)])), total, smap, out_blocks=blocks)
+        assert host(blocks).tolist() == [r + [-1] * (W - len(r)) for r in rb] and host(smap).tolist() == [x for r in rm for x in r]
+        assert int(pool.state[1]) == 0 and pool.status() == (E.ELIS_OK, 0)
+    pool.trim(i32(slots), i32(np.zeros(n)))
+    assert host(pool.free_pages).tolist() == list(range(int(need.sum())))[::-1] and int(pool.held.sum()) == 0
+
+
 # ------------------------------------------------------------------ the cache
 
 def filled(rng, T, heads, d, extra=0):
@@ -159,6 +180,9 @@ def test_append_ties_and_non_finite():
         assert np.array_equal(host(o), O.kv_round(host(t)), equal_nan=True)
     note("kv append / read: a slot outside the cache")
     cache.append(t, t, i32([16, -1, 2 ** 31 - 1]))
+    assert cache.status() == (E.ELIS_EDEVICE, E.ELIS_DEV_BAD_PAGE)
+    E.check(E.elis_kv_init(cache.c, None))
+    cache.append(t, t, i32([-1, -7, -1]))
     assert cache.status() == (E.ELIS_EDEVICE, E.ELIS_DEV_BAD_PAGE)
     cache.read(i32([99, -1, 3]), *out)
     assert (host(out[0])[:2] == 0).all() and np.array_equal(host(out[0])[2], O.kv_round(host(t[0])))
@@ -256,6 +280,89 @@ def test_attention_of_many_rows(heads, kv_heads, d, window, q_lens, kv_lens):
     out = cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(blocks), max(q_lens), max(kv_lens), window=window)
     assert cache.status() == (E.ELIS_OK, 0)
     check_attention(out, q, q_lens, kv_lens, k, v, d ** -0.5, window)
+
+
+@pytest.mark.parametrize("q_lens,room", [([40, 1], 40), ([0, 40, 3], 27), ([1, 40, 0, 12], 67)])
+def test_attention_of_padded_rows(q_lens, room):
+    """As many rows as if every request had max_q tokens, though some are shorter and the last rows are nobody's."""
+    rng = np.random.default_rng(len(q_lens))
+    T, kv_lens = sum(q_lens), [n + 20 for n in q_lens]
+    note(f"kv attention padded q={q_lens} rows {T + room}")
+    cache, blocks, k, v, _ = paged(rng, kv_lens, 2, 64, 16)
+    for n in (len(q_lens) * 40, T + room):
+        q = torch.from_numpy(rng.standard_normal((n, 4, 64))).to("cuda").to(BF)
+        out = torch.full_like(q, 5.0)
+        cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(blocks), 40, max(kv_lens), out=out)
+        check_attention(out, q, q_lens, kv_lens, k, v, 64 ** -0.5)
+        assert (host(out)[T:] == 5).all()
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([1], [9001]), ([1, 1, 3, 1], [9001, 20, 5300, 2000]), ([80, 1, 2], [7000, 9001, 1])])
+@pytest.mark.parametrize("window", [1500, 5000, 9000, 2 ** 31 - 1])
+def test_attention_of_long_windows(q_lens, kv_lens, window):
+    rng = np.random.default_rng(window % 1000)
+    note(f"kv attention q={q_lens} kv={kv_lens} window={window}")
+    cache, blocks, k, v, _ = paged(rng, kv_lens, 1, 64, 32)
+    q = torch.from_numpy(rng.standard_normal((sum(q_lens), 4, 64))).to("cuda").to(BF)
+    out = cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(blocks), max(q_lens), max(kv_lens), window=window)
+    check_attention(out, q, q_lens, kv_lens, k, v, 64 ** -0.5, window)
+
+
+def test_attention_of_no_tokens_and_of_more_than_there_are_keys():
+    rng = np.random.default_rng(6)
+    cache, blocks, k, v, _ = paged(rng, [2, 5], 1, 64, 16)
+    note("kv attention of no tokens")
+    assert cache.attention(torch.empty((0, 2, 64), dtype=BF, device="cuda"), i32([0, 0, 0]), i32([2, 5]), i32(blocks), 1, 5).shape == (0, 2, 64)
+    for window in (0, 1, 3, 2 ** 31 - 1):
+        note(f"kv attention of more tokens than keys, window {window}")
+        q = torch.from_numpy(rng.standard_normal((13, 2, 64))).to("cuda").to(BF)
+        out = cache.attention(q, i32([0, 4, 13]), i32([2, 5]), i32(blocks), 9, 5, window=window)
+        check_attention(out, q, [4, 9], [2, 5], k, v, 64 ** -0.5, window)
+
+
+def test_attention_on_two_streams_and_in_two_graphs():
+    """One cache, calls that split their keys: on two streams at once, and in two graphs replayed in turn with eager calls
+    of other sizes between them."""
+    rng = np.random.default_rng(12)
+    kv = [9001, 4000, 5200]
+    cache, blocks, k, v, _ = paged(rng, kv, 2, 64, 16)
+    blocks, at = i32(blocks), np.concatenate([[0], np.cumsum(kv)])
+
+    def check(out, q, which):
+        pick = np.concatenate([np.arange(at[i], at[i + 1]) for i in which])
+        check_attention(out, q, [1] * len(which), [kv[i] for i in which], k[pick], v[pick], 64 ** -0.5)
+
+    sets = ([0], [1, 2], [2, 0, 1])
+    q = [torch.from_numpy(rng.standard_normal((len(w), 4, 64))).to("cuda").to(BF) for w in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    note("kv attention on three streams")
+    args = [(i32(np.arange(len(w) + 1)), i32([kv[i] for i in w]), blocks[w].contiguous(), 1, max(kv[i] for i in w)) for w in sets]
+    torch.cuda.synchronize()
+    outs = []
+    for turn in range(5):
+        for s, x, a in zip(streams, q, args):
+            outs.append(cache.attention(x, *a, stream=s if turn % 2 else s.cuda_stream))
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        check(out, q[i % 3], sets[i % 3])
+    note("kv attention in two graphs")
+    graphs, held = [], [torch.zeros_like(x) for x in q[:2]]
+    for x, a, o in zip(q, args, held):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cache.attention(x, *a, out=o)
+        graphs.append(g)
+    for replay in range(4):
+        for x in q:
+            x.copy_(torch.from_numpy(rng.standard_normal(tuple(x.shape))).to("cuda"))
+        for o in held:
+            o.fill_(9)
+        graphs[replay % 2].replay()
+        eager = cache.attention(q[2], *args[2])
+        graphs[1 - replay % 2].replay()
+        torch.cuda.synchronize()
+        for o, x, w in zip((*held, eager), q, sets):
+            check(o, x, w)
 
 
 def test_cache_past_four_gib():
