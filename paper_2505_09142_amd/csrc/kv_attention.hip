@@ -286,7 +286,7 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
     auto load_k = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
         if constexpr (D == 128) x.k[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lk, 0, 0);
         else x.k[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lk, 0, 0);
-        x.ks[u] = __builtin_amdgcn_raw_buffer_load_b8(rec, lks, 0, 0);
+        x.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lks & ~3u, 0, 0);
     };
     auto load_v = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
         if constexpr (D == 128) x.v[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lv, 0, 0);
@@ -393,7 +393,7 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
 #pragma unroll
                     for (int u = 0; u < UB; ++u) {
                         const uint32_t w = x.k[u0 + u][t];
-                        const float ksc = __uint_as_float(x.ks[u0 + u] << 23);
+                        const float ksc = scale_of(x.ks[u0 + u], lks & 3);
                         const u32x4 kk = {two_values<0>(w, ksc), two_values<1>(w, ksc), two_values<2>(w, ksc), two_values<3>(w, ksc)};
 #pragma unroll
                         for (int j = 0; j < NB; ++j)

@@ -19,7 +19,8 @@ namespace elis {
 namespace {
 
 constexpr int kScan = 1024;   // threads of the scan
-constexpr int kEach = 2;      // entries a thread of it holds at a time (2,048 entries: 1 / 2 / 4 of them 11.2 / 10.7 / 12.0 us)
+constexpr int kEach = 2;      // entries a thread of it holds at a time (grow and trim of 200 entries: 1 / 2 / 4 of them 11.0 / 11.7 /
+                              // 13.3 us, of 2,048: 21.1 / 20.0 / 22.1, of 20,000: 152 / 138 / 150)
 constexpr int kSmall = 128;   // entries up to which one launch does all,
 constexpr int kSmallWork = 32768;  // with at most so many cells and slots to write
 constexpr int kFill = 256;    // threads of a work-group of the second launch
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
             const bool fits = move == 0 || incl <= count;
             if (!fits) bad |= ELIS_DEV_NO_PAGES;
             else h1 = h0 + move;
-            if (move > 0 && fits) atomicMax(&taken_s, incl);
+            if (total > count && move > 0 && fits) atomicMax(&taken_s, incl);
             first[i] = count - 1 - (incl - move);
         } else {
             h1 = h0 - move;
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
     if (bad) atomicOr(&bad_s, bad);
     __syncthreads();
     if (tid == 0) {
-        const int now = GROW ? count - taken_s : count + total;
+        const int now = GROW ? count - (total > count ? taken_s : total) : count + total;
         a.p.state[1] = now < a.p.n_pages ? now : a.p.n_pages;
         if (bad_s) atomicOr(reinterpret_cast<uint32_t*>(&a.p.state[0]), bad_s);
     }
@@ -340,11 +341,12 @@ __global__ __launch_bounds__(kScan) void pages_scan_kernel(FillArgs a) {
         }
         __syncthreads();  // wave_tot is free
     }
-    if (taken) atomicMax(&taken_s, taken);
+    // Where the free pages reach for all, they are the sum; a maximum over 1,024 threads costs 3.5 us.
+    if (carry > count && taken) atomicMax(&taken_s, taken);
     if (bad) atomicOr(&bad_s, bad);
     __syncthreads();
     if (tid == 0) {
-        const int now = GROW ? count - taken_s : count + carry;
+        const int now = GROW ? count - (carry > count ? taken_s : carry) : count + carry;
         a.p.state[1] = now < a.p.n_pages ? now : a.p.n_pages;
         if (!GROW) a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)] = carry;
         if (bad_s) atomicOr(reinterpret_cast<uint32_t*>(&a.p.state[0]), bad_s);
