@@ -748,7 +748,7 @@ int check_kv_attention_sizes(int32_t n, int32_t total_q, int32_t max_q, int32_t 
     if (static_cast<int64_t>(max_q) * (n_heads / n_kv_heads) > INT32_MAX / 128 ||
         static_cast<int64_t>(total_q) * n_heads > INT32_MAX / 64)
         return ELIS_ESHAPE;
-    if (kv_attention_work_groups(plan_kv_attention(n, total_q, max_q, max_kv, n_heads, n_kv_heads, 0), n, n_kv_heads) > INT32_MAX / 256)
+    if (kv_attention_work_groups(plan_kv_attention(n, total_q, max_q, max_kv, n_heads, n_kv_heads, d_head, 0), n, n_kv_heads) > INT32_MAX / 256)
         return ELIS_ESHAPE;
     return ELIS_OK;
 }
@@ -826,7 +826,7 @@ int elis_kv_read(const elis_kv_cache* c, const int32_t* slot_map, int32_t n_toke
 size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                          int32_t n_kv_heads, int32_t d_head) {
     if (check_kv_attention_sizes(n, total_q, max_q, max_kv, n_heads, n_kv_heads, d_head) != ELIS_OK) return 0;
-    return kv_attention_ws(plan_kv_attention(n, total_q, max_q, max_kv, n_heads, n_kv_heads, 0), d_head);
+    return kv_attention_ws(plan_kv_attention(n, total_q, max_q, max_kv, n_heads, n_kv_heads, d_head, 0), d_head);
 }
 
 int elis_kv_attention(const elis_kv_cache* c, const uint16_t* q, int64_t q_stride, const int32_t* cu_q, int32_t n,
@@ -844,7 +844,7 @@ int elis_kv_attention(const elis_kv_cache* c, const uint16_t* q, int64_t q_strid
     if (q_stride < row || out_stride < row || static_cast<int64_t>(blocks_stride) * c->page_tokens < max_kv || (!rows && block_rows < n))
         return ELIS_ESHAPE;
     if (window >= max_kv) window = 0;  // every key before a token is in it (and positions less a window stay in range)
-    const KvAttnPlan p = plan_kv_attention(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads, window);
+    const KvAttnPlan p = plan_kv_attention(n, total_q, max_q, max_kv, n_heads, c->n_kv_heads, c->d_head, window);
     if (ws_bytes < kv_attention_ws(p, c->d_head)) return ELIS_EWORKSPACE;
     if (total_q == 0) return ELIS_OK;
     KvAttnArgs a{};

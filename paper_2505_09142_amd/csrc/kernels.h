@@ -192,7 +192,7 @@ struct KvAttnPlan {
     long long small_most, many_most;  // chunks at most, with any window
     size_t small_parts, many_parts;  // chunk results to join (d_head floats and two more each)
 };
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int window);
+KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int d_head, int window);
 long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads);
 struct KvAttnArgs {
     KvCacheView c;

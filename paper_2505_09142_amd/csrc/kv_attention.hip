@@ -27,7 +27,8 @@
 // Bounds. Single tokens: memory, 17/16 D bytes a key and kv head, once (48 requests of 16,000 tokens and 8 kv heads of 128:
 // 207 us, 5.0 TB/s, more than a copy reaches). Long prompts: the vector unit, which unpacks and takes exponentials beside
 // the products (2,048 tokens of 32 heads over 16,000 keys: 484 us, 1.04 PFLOP/s; vector unit busy 65 % of it, matrix unit
-// 41 %). One request alone: latency. Its keys are split (chunks) and joined by a second launch.
+// 41 %; they overlap little: two waves' 64 products and 232 vector instructions each take 1.7 us where either kind alone
+// takes 0.9 and 1.1, and the kernel's 64 and 270 take 2.0). One request alone: latency. Its keys are split (chunks) and joined by a second launch.
 #include <math.h>
 
 #include <type_traits>
@@ -41,7 +42,6 @@ namespace {
 constexpr int kStep = 32;  // keys a wave takes at a time: two records
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr unsigned kMixedMost = 2048;  // work-groups of short requests up to which they run beside the long ones'
 constexpr float kLowest = -3.0e38f;  // a maximum over no keys: finite, so that differences of maxima are numbers
 constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
 
@@ -618,7 +618,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(NB)) void kv_attention_ker
     attend<D, NB, MANY>(a, blockIdx.x, sh);
 }
 
-// Both at once, the long requests' tiles first: neither waits for the other's last work-groups.
+// Both at once: neither waits for the other's last work-groups. The long requests' tiles come first, the single tokens fill
+// in behind (two prompts of up to 512 tokens beside 30 tokens: 37 us, the tokens among the tiles 43, before them 42).
 template <int D, int NB, int NBM>
 __global__ __launch_bounds__(kThreads, waves_per_simd(NBM)) void kv_attention_mixed_kernel(KvAttnArgs a, KvAttnMany m) {
     union Both {
@@ -721,6 +722,9 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
 }
 
 template <int D>
+constexpr int kNbMost = D == 128 ? 4 : 2;
+
+template <int D>
 hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
     KvAttnArgs a = args;  // as the short requests' launch takes it
     a.nchunks = p.small_chunks;
@@ -728,19 +732,16 @@ hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
     const unsigned heads = static_cast<unsigned>(a.c.n_kv_heads);
     const unsigned small = p.small_rows > 0 ? heads * a.n * p.small_chunks : 0, many = heads * p.many_tiles * p.many_chunks;
     const KvAttnMany m{static_cast<int>(many), p.many_chunk, p.many_chunks, 16 * p.many_nb, p.small_parts};  // both may have chunk results at once
-    if (small && many && small <= kMixedMost) {
-        const auto f = p.small_nb == 2 ? (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 2, 4> : kv_attention_mixed_kernel<D, 2, 2>)
-                                       : (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 1, 4> : kv_attention_mixed_kernel<D, 1, 2>);
+    if (small && many) {
+        const auto f = p.small_nb == 2 ? (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 2, kNbMost<D>> : kv_attention_mixed_kernel<D, 2, 2>)
+                                       : (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 1, kNbMost<D>> : kv_attention_mixed_kernel<D, 1, 2>);
         ELIS_TRY(launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, m));
-    } else {
-        if (small) {
-            const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : kv_attention_kernel<D, 2, false>;
-            ELIS_TRY(launch_kernel(f, dim3(small), dim3(kThreads), 0, st, a));
-        }
-        if (many) {
-            const auto f = p.many_nb == 2 ? kv_attention_kernel<D, 2, true> : kv_attention_kernel<D, 4, true>;
-            ELIS_TRY(launch_kernel(f, dim3(many), dim3(kThreads), 0, st, m.of(a, D)));
-        }
+    } else if (small) {
+        const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : kv_attention_kernel<D, 2, false>;
+        ELIS_TRY(launch_kernel(f, dim3(small), dim3(kThreads), 0, st, a));
+    } else if (many) {
+        const auto f = p.many_nb == 2 ? kv_attention_kernel<D, 2, true> : kv_attention_kernel<D, kNbMost<D>, true>;
+        ELIS_TRY(launch_kernel(f, dim3(many), dim3(kThreads), 0, st, m.of(a, D)));
     }
     const long long small_joins = small && p.small_chunks > 1 ? static_cast<long long>(heads) * a.n * p.small_rows : 0;
     const long long joins = small_joins + (many && p.many_chunks > 1 ? static_cast<long long>(a.total_q) * a.n_heads : 0);
@@ -758,12 +759,20 @@ long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 // Short requests: chunks. A work-group needs about 4.5 us whatever its keys and 0.5 us for each 128, and joining costs 4
 // us, so up to 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001
 // tokens and 8 kv heads: chunks of 512 / 1,024 / 2,048 keys 16.9 / 15.4 / 19.0 us), and at least three to a request that is
-// as long as max_kv, because the others are shorter (64 requests of up to 3,872 tokens: one chunk 25.3, chunks of 1,024
-// 23.5), but not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 /
-// 206). Long requests: tiles of 64 rows where they fill the machine twice (2,048 tokens of 32 heads over 16,000 keys: 483 us,
-// tiles of 32 rows 536), else of 32, of which a CU runs three and whose steps take 0.75 us for 1.6 (2 x 185 tokens of 20
-// heads over 2,676 keys 42 and 26 us); where their rows are more than 1,024, joining costs more, and only half a fill is split.
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int window) {
+// as long as max_kv, because the others are shorter (one chunk, three and six of them: 64 requests of up to 3,872 tokens
+// 23.9 / 23.1 / 24.1, 90 of up to 9,000 44.8 / 38.8 / 39.3, but 64 of up to 1,900 with 12 heads of 64 15.3 / 18.6 / 20.0: the
+// join), but not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 /
+// 206).
+//
+// Long requests: tiles of 32 rows, of which a CU runs three at a time, a 128-key round of theirs in 1.5 us; or, with heads
+// of 128, of 64 rows, two at a time in 2.05. What counts is how many fills of the 256 CUs they take, at 3 : 4 (tokens of 32
+// query and 8 kv heads over 9,000 keys: 512 tokens 32 rows 101 us, 64 rows 118; 1,000 165, 147; 1,500 227, 262; 2,048 290,
+// 265), if the tiles have about the same keys and single tokens do not fill the gaps (four prompts of 1,024 tokens with no
+// keys before them 63 and 67; prompts of up to 900 beside 8 tokens 168 and 182). They are split over the keys where they do
+// not fill the machine (two of 185 tokens of 20 heads over 2,676 keys 42 and 26 us; 100 tokens of 8 heads over 9,000: 62 and
+// 21); of more than 1,024 rows only up to half a fill, because joining costs more (of 8 heads over 9,000 keys, half and whole
+// fill: 200 tokens 30.5 and 29.0, 500 43.0 and 45.8).
+KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int d_head, int window) {
     KvAttnPlan p{};
     const int group = n_heads / n_kv_heads;
     const long long most = static_cast<long long>(max_q) * group;
@@ -801,7 +810,9 @@ KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_he
     p.many_chunks = 1;
     if (p.many) {
         const long long rows = static_cast<long long>(total_q) * group, longer = rows / (p.small + 1);
-        p.many_nb = (rows / 64 + 1) * n_kv_heads < 1024 ? 2 : 4;
+        const long long t4 = (rows + 63) / 64 * n_kv_heads, t2 = (rows + 31) / 32 * n_kv_heads;
+        const bool alone = p.small_rows == 0 || 4LL * n * n_kv_heads * small_most <= t4, even = max_kv > 2LL * max_q;
+        p.many_nb = d_head == 128 && alone && even && 4 * ((t4 + 511) / 512) < 3 * ((t2 + 767) / 768) ? 4 : 2;
         const int tile = 16 * p.many_nb;
         p.many_tiles = static_cast<int>(rows / tile + (longer < n ? longer : n));  // at most: every long request's last tile cut
         const long long per = (rows / tile + 1) * n_kv_heads;

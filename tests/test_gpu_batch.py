@@ -365,6 +365,29 @@ def test_attention_on_two_streams_and_in_two_graphs():
             check(o, x, w)
 
 
+@pytest.mark.parametrize("heads,kv_heads,q_lens,kv_lens,window", [
+    (128, 128, [200], [450], 0), (128, 128, [200], [450], 70),       # tiles of 64 rows, alone
+    (64, 64, [448, 1], [1000, 300], 0), (64, 64, [448, 1], [1000, 300], 129),  # beside a single token
+    (160, 8, [158, 1, 1], [400, 50, 70], 0),                          # beside single tokens of 20 rows
+    (128, 128, [230], [4700], 0)])                                    # keys past what the lanes hold pages for
+def test_attention_in_tall_tiles(heads, kv_heads, q_lens, kv_lens, window):
+    """Few enough tiles of 64 rows for one fill of the machine, too many of 32."""
+    note(f"kv attention q={q_lens} kv={kv_lens} heads={heads}/{kv_heads} window={window}")
+    rng = np.random.default_rng(heads + len(q_lens))
+    cache, blocks, k, v, _ = paged(rng, kv_lens, kv_heads, 128, 16)
+    T = sum(q_lens)
+    q = torch.from_numpy(rng.standard_normal((T + 1, heads, 128))).to("cuda").to(BF)
+    out = torch.full_like(q, 5.0)
+    cu = i32(np.concatenate([[0], np.cumsum(q_lens)]))
+    for rows in (T, T + 1):
+        cache.attention(q[:rows], cu, i32(kv_lens), i32(blocks), max(q_lens), max(kv_lens), window=window, out=out[:rows])
+        assert cache.status() == (E.ELIS_OK, 0)
+        few = [0, 5, kv_heads - 1] if heads == kv_heads else range(kv_heads)  # the oracle takes a minute for all of 128
+        qh = [h * heads // kv_heads + i for h in few for i in range(heads // kv_heads)]
+        check_attention(out[:, qh], q[:, qh], q_lens, kv_lens, k[:, list(few)], v[:, list(few)], 128 ** -0.5, window)
+        assert (host(out)[T:] == 5).all() and np.isfinite(host(out)).all()
+
+
 def test_cache_past_four_gib():
     """Records whose places pass 32 bits: append, read and attention on the last pages of a large cache."""
     rng = np.random.default_rng(4)
