@@ -735,7 +735,7 @@ int check_kv_rows(const elis_kv_cache* c, const void* k, const void* v, int64_t 
     if (n_tokens < 0 || (n_tokens > 0 && (!k || !v || !slot_map))) return ELIS_EINVAL;
     const int64_t row = static_cast<int64_t>(c->n_kv_heads) * c->d_head;
     if (k_stride < row || v_stride < row) return ELIS_ESHAPE;
-    if ((static_cast<int64_t>(n_tokens) + 3) / 4 * 4 * row / 8 > INT32_MAX) return ELIS_ESHAPE;
+    if ((static_cast<int64_t>(n_tokens) + kKvTogether - 1) / kKvTogether * kKvTogether * row / 8 > INT32_MAX) return ELIS_ESHAPE;
     return ELIS_OK;
 }
 

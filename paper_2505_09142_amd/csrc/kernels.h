@@ -176,6 +176,7 @@ struct KvCacheView {
     uint8_t* pages;
     int n_pages, page_tokens, page_shift, n_kv_heads, d_head;
 };
+constexpr int kKvTogether = 16;  // tokens of a head that a launch takes together
 hipError_t launch_kv_init(KvCacheView c, hipStream_t st);
 // Strides in elements from token to token.
 hipError_t launch_kv_append(KvCacheView c, const uint16_t* k, const uint16_t* v, long long k_stride, long long v_stride, const int32_t* map, int n,

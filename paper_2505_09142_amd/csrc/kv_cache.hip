@@ -7,8 +7,11 @@
 // computed; the conversion instructions (v_cvt_scalef32_pk_fp4_bf16, v_cvt_scalef32_pk_bf16_fp4) are exact here.
 //
 // Bound by memory: 4 D bytes of bf16 in and 17/16 D out a token and head (read: the reverse). A lane holds 8 values of
-// a key row and of the value row (16 bytes each); four lanes share a scale. The lanes of a wave cover four tokens of
-// one head, whose value words are interleaved in the record, so an aligned group of four writes whole lines.
+// a key row and of the value row (16 bytes each); four lanes share a scale. A work-group's lanes cover 16 tokens (D 64: of
+// two heads) before the next head: nearly always a record or two, whose lines then fill in one L2 before they leave it (32,768
+// tokens of 8 heads of 128, append and read: 4 / 8 / 16 / 32 tokens 78.7 / 74.8 / 71.9 / 74.3 us; with 4 the append wrote 1.4
+// times its bytes). What is read goes past the L2 (non-temporal stores, 71.9 -> 62.8; of the inputs too: 61.8, but 500 tokens
+// 4.95 -> 5.35). A copy of the same bytes would take 72.
 #include "kv_cache.h"
 
 namespace elis {
@@ -87,7 +90,7 @@ __device__ __forceinline__ u32x4 load8(const uint16_t* p) {
 template <bool VEC>
 __device__ __forceinline__ void store8(uint16_t* p, u32x4 x) {
     if constexpr (VEC) {
-        *reinterpret_cast<u32x4*>(p) = x;
+        __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -97,16 +100,16 @@ __device__ __forceinline__ void store8(uint16_t* p, u32x4 x) {
     }
 }
 
-// Unit u of a call: lane part `sub` (8 values) of token t and head h; the tokens of a group of four are adjacent.
+// Unit u of a call: lane part `sub` (8 values) of token t and head h; kKvTogether tokens are adjacent.
 template <int D>
 __device__ __forceinline__ void unit_of(long long u, int heads, long long* t, int* h, int* sub) {
     constexpr int L = D / 8;
     *sub = static_cast<int>(u % L);
     u /= L;
-    const int b = static_cast<int>(u & 3);
-    u >>= 2;
+    const int b = static_cast<int>(u % kKvTogether);
+    u /= kKvTogether;
     *h = static_cast<int>(u % heads);
-    *t = u / heads * 4 + b;
+    *t = u / heads * kKvTogether + b;
 }
 
 template <int D, bool VEC>
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCacheView c, const 
 }
 
 dim3 grid_for(const KvCacheView& c, int n) {
-    const long long units = (static_cast<long long>(n) + 3) / 4 * 4 * c.n_kv_heads * (c.d_head / 8);
+    const long long units = (static_cast<long long>(n) + kKvTogether - 1) / kKvTogether * kKvTogether * c.n_kv_heads * (c.d_head / 8);
     return dim3(static_cast<unsigned>((units + kThreads - 1) / kThreads));
 }
 

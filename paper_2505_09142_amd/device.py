@@ -200,7 +200,7 @@ def _dev() -> int:
 
 def _arg(t: torch.Tensor, dtype: torch.dtype, dev: int, where: str, at_least: int = 0) -> int:
     """Address of a contiguous argument of the given type, on device `dev`, of at least so many elements."""
-    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < at_least:
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or (at_least and t.numel() < at_least):
         raise E.ElisError(E.ELIS_EINVAL, where)
     return t.data_ptr()
 
@@ -301,6 +301,7 @@ class KVCache:
         self.buf, self.dev = buf, buf.get_device()
         self.c = E.elis_kv_cache(base, n_pages, page_tokens, n_kv_heads, d_head)
         self.ws = Workspace(buf.device)
+        self._no_ws = self.ws.get(256)[0]
         self._sizes, self._need = None, 0  # of the last attention call, and the workspace they take
         if made:
             _made_on(self.dev, "elis_kv_init")
@@ -347,9 +348,9 @@ class KVCache:
         sizes = (n, total, max_q, max_kv, heads)
         if sizes != self._sizes:
             self._need, self._sizes = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d), sizes
-        # A workspace of the call's own: calls on several streams, and captured graphs, share none but the one that holds
+        # A workspace of the call's own: calls on several streams, and captured graphs, share only the one that holds
         # nothing (256 bytes, not touched).
-        (ws, _), wsb = self.ws.get(256), self._need
+        ws, wsb = self._no_ws, self._need
         if wsb > 256:
             with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream)):
                 scratch = torch.empty(wsb + 256, dtype=torch.uint8, device=q.device)
