@@ -14,6 +14,7 @@ import torch
 
 from . import _elis as E
 
+I32, F32, BF16 = torch.int32, torch.float32, torch.bfloat16
 BF16_KEYS = ("word", "pos", "w_qkv", "w_o", "w_1", "w_2")
 
 
@@ -217,7 +218,7 @@ def _opt(t: torch.Tensor | None, dtype: torch.dtype, dev: int, where: str, at_le
 
 def _heads(x: torch.Tensor, tokens: int, heads: int, d: int, dev: int, where: str) -> int:
     """Token stride of a [tokens, heads, d] or [tokens, heads * d] bf16 tensor whose rows are contiguous."""
-    if x.dtype is not torch.bfloat16 or x.get_device() != dev:
+    if x.dtype is not BF16 or x.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
     shape, stride = x.shape, x.stride()
     if shape == (tokens, heads, d):
@@ -261,7 +262,7 @@ class PagePool:
              out_slot_map: torch.Tensor | None, out_blocks: torch.Tensor | None = None, stream=None):
         """Pages for lens[i] tokens of job slots[i]; the slots of the step's total_new new tokens into out_slot_map
         and, if given, the batch's block table into out_blocks [n, width]."""
-        n, i32, dev, where = slots.numel(), torch.int32, self.state.get_device(), "elis_pages_grow"
+        n, i32, dev, where = slots.numel(), I32, self.state.get_device(), "elis_pages_grow"
         if dev != _dev():
             raise E.ElisError(E.ELIS_EINVAL, where)
         if out_blocks is not None and (out_blocks.dim() != 2 or out_blocks.shape[0] != n):
@@ -335,7 +336,7 @@ class KVCache:
                   out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Causal attention of the new tokens q (bf16 [tokens, n_heads, d_head]) over the cache. ``blocks`` holds a
         row of page ids for every request, or, with ``rows``, for every job slot (a pool's table)."""
-        n, i32, where = kv_lens.numel(), torch.int32, "elis_kv_attention"
+        n, i32, where = kv_lens.numel(), I32, "elis_kv_attention"
         dev = self._here(where)
         if q.dim() != 3 or blocks.dim() != 2:
             raise E.ElisError(E.ELIS_ESHAPE, where)
@@ -372,15 +373,15 @@ def adjust_logits(logits: torch.Tensor, token_ids: torch.Tensor | None, cu_seqle
     """elis_logits_adjust on [n, vocab] logits (bf16 or fp32, rows contiguous). token_ids / cu_seqlens: the histories
     as JobTable.pack writes them. bias: (cu [n + 1], tokens, values). mask: int32 or uint32 [n_masks, words]."""
     where, dev = "elis_logits_adjust", _dev()
-    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1 or \
+    if logits.dim() != 2 or (logits.dtype is not F32 and logits.dtype is not BF16) or logits.stride(1) != 1 or \
             logits.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
     n, vocab = logits.shape
     if out is None:
         out = torch.empty((n, vocab), dtype=torch.float32, device=logits.device)
-    if out.shape != logits.shape or out.dtype is not torch.float32 or out.stride(1) != 1 or out.get_device() != dev:
+    if out.shape != logits.shape or out.dtype is not F32 or out.stride(1) != 1 or out.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
-    f32, i32 = torch.float32, torch.int32
+    f32, i32 = F32, I32
     b_cu, b_tok, b_val = bias if bias is not None else (None, None, None)
     total = 0 if token_ids is None else token_ids.numel()
     n_bias = 0 if b_tok is None else b_tok.numel()

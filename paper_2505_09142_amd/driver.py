@@ -215,6 +215,8 @@ class DeviceRoundDriver:
         """Pages for the jobs' lens tokens, in the order of the call (the selection's: the first jobs are served first
         when pages run out). With `new`, the last new[i] of job i's tokens are this step's: their cache slots go into
         out_slot_map. Returns the jobs' slots, the rows of the pool's table, on the device (valid until the next call)."""
+        if len(lens) != len(jobs):
+            raise ValueError("one length for each job")
         cu = np.zeros(len(jobs) + 1, dtype=np.int32)
         if new is not None:
             np.cumsum(new, out=cu[1:])
@@ -233,11 +235,13 @@ class DeviceRoundDriver:
         """device.adjust_logits on one row of logits a job, with the tokens that the table holds as its history (past
         max_pos tokens the first one and the most recent max_pos - 1). The other arguments are passed on."""
         n = len(jobs)
-        if logits.dim() != 2 or logits.shape[0] != n:
-            raise ValueError("one row of logits for each job")
+        if logits.dim() != 2 or logits.shape[0] != n or len(prompt_lens) != n:
+            raise ValueError("one row of logits and one prompt length for each job")
         if n == 0:
             return adjust_logits(logits, None, None, out)
         total = np.fromiter((self.appended[j] for j in jobs), dtype=np.int64, count=n)
+        if total.min() < 1:
+            raise ValueError("a job without tokens")
         held = np.minimum(total, self.max_pos)
         # of a longer history the first token and those from `tail` on are held: so many of them are the prompt's
         plen, tail = np.asarray(prompt_lens, dtype=np.int64), total - (self.max_pos - 1)

@@ -86,3 +86,21 @@ def test_slot_maps_and_logits_of_a_batch():
     drv.drop([5])
     drv.release([3, 11, 8])
     assert int(drv.pages.state[1]) == 64 and drv.table.status() == (E.ELIS_OK, 0)
+
+
+def test_batches_that_are_refused_or_empty():
+    drv = DeviceRoundDriver(None, 8, 16, pages=PagePool(8, 16, 8, 4))
+    drv.start([1, 2], [0, 1])
+    note("driver: empty and refused batches")
+    drv.sync_tokens([1], {1: np.array([4, 5], dtype=np.int32)}, {1: np.zeros(0, np.int32)}, {1: 0})
+    logits = torch.zeros((2, 9), device="cuda")
+    for jobs, prompts in (([1, 2], [2, 1]), ([1], [2]), ([1, 1], [2])):  # a job without tokens; rows or lengths that do not fit
+        with pytest.raises(ValueError):
+            drv.adjust_logits(jobs, logits, prompts)
+    assert drv.table.status() == (E.ELIS_OK, 0)
+    with pytest.raises(ValueError):
+        drv.reserve([1, 2], [5])
+    assert drv.reserve([], []).numel() == 0
+    drv.reserve([2], [33])
+    drv.drop([])
+    assert int(drv.pages.state[1]) == 5 and drv.pages.status() == (E.ELIS_OK, 0)
