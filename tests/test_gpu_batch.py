@@ -388,6 +388,62 @@ def test_attention_in_tall_tiles(heads, kv_heads, q_lens, kv_lens, window):
         assert (host(out)[T:] == 5).all() and np.isfinite(host(out)).all()
 
 
+@pytest.mark.parametrize("longest", [1, 40])
+@pytest.mark.parametrize("window", [0, 9])
+def test_attention_of_many_requests(longest, window):
+    """More requests than a work-group has threads, some of them empty, with lengths in no order."""
+    rng = np.random.default_rng(longest)
+    n = 700
+    q_lens = rng.integers(0, longest + 1, n)
+    kv_lens = (q_lens + rng.integers(0, 30, n)).tolist()
+    q_lens[[0, 300, n - 1]], kv_lens[5] = [0, longest, longest], 2000
+    kv_lens = np.maximum(kv_lens, q_lens).tolist()
+    note(f"kv attention of {n} requests of up to {longest} tokens, window {window}")
+    cache, blocks, k, v, _ = paged(rng, kv_lens, 1, 64, 16)
+    q = torch.from_numpy(rng.standard_normal((int(q_lens.sum()), 2, 64))).to("cuda").to(BF)
+    out = cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(blocks), longest, max(kv_lens), window=window)
+    assert cache.status() == (E.ELIS_OK, 0)
+    check_attention(out, q, q_lens.tolist(), kv_lens, k, v, 64 ** -0.5, window)
+
+
+def test_wrappers_refuse_what_does_not_fit():
+    """Tensors of another device, type, shape or layout never reach a kernel."""
+    note("refusals of the wrappers")
+    pool, cache = PagePool(8, 16, 4, 3), KVCache(8, 16, 2, 64)
+    s, cu, m = i32([0, 1]), i32([0, 3, 5]), i32([0] * 5)
+    kv, q = torch.zeros((5, 2, 64), dtype=BF, device="cuda"), torch.zeros((5, 4, 64), dtype=BF, device="cuda")
+    lens, blocks = i32([3, 2]), i32([[0], [1]])
+    x, ids = torch.zeros((2, 50), device="cuda"), i32([1, 2, 3, 4, 5])
+    calls = [
+        lambda: pool.grow(s.cpu(), lens, cu, 5, m), lambda: pool.grow(s.long(), lens, cu, 5, m), lambda: pool.grow(s, lens[:1], cu, 5, m),
+        lambda: pool.grow(s, lens, cu[:2], 5, m), lambda: pool.grow(s, lens, cu, 6, m), lambda: pool.grow(s, lens, cu, 5, m, out_blocks=blocks[:1]),
+        lambda: pool.grow(s, lens, cu, 5, i32([[0, 0]] * 5)[:, 0]), lambda: pool.grow(i32([0, 1, 2, 3, 0]), i32([1] * 5), i32(range(6)), 5, m),
+        lambda: pool.grow(s, lens, None, 5, m), lambda: pool.grow(s, lens, cu, 5, m, out_blocks=i32([[0] * 4] * 2)),
+        lambda: pool.trim(s, lens.cpu()), lambda: pool.trim(s, lens[:1]),
+        lambda: cache.append(kv.float(), kv, m), lambda: cache.append(kv[:4], kv, m), lambda: cache.append(kv, kv.cpu(), m),
+        lambda: cache.append(kv[:, :1], kv, m), lambda: cache.append(kv.transpose(1, 2).contiguous().transpose(1, 2), kv, m),
+        lambda: cache.append(kv[:1].expand(5, 2, 64), kv, m), lambda: cache.append(kv, kv, m.long()), lambda: cache.read(m, kv, kv.half()),
+        lambda: cache.attention(q.half(), cu, lens, blocks, 3, 3), lambda: cache.attention(q[:, :3], cu, lens, blocks, 3, 3),
+        lambda: cache.attention(q, cu[:2], lens, blocks, 3, 3), lambda: cache.attention(q, cu, lens, blocks[0], 3, 3),
+        lambda: cache.attention(q, cu, lens, blocks.cpu(), 3, 3), lambda: cache.attention(q, cu, lens, blocks, 3, 17),
+        lambda: cache.attention(q, cu, lens, blocks[:1], 3, 3), lambda: cache.attention(q, cu, lens, blocks, 3, 3, rows=s[:1]),
+        lambda: cache.attention(q, cu, lens, blocks, 3, 3, out=q[:3]), lambda: cache.attention(q, cu, lens, blocks, 3, 3, scale=-1.0),
+        lambda: cache.attention(q, cu, lens, blocks, 0, 3), lambda: cache.attention(q, cu, lens, i32([[0, 9], [1, 9]])[:, :1], 3, 3),
+        lambda: adjust_logits(x.cpu(), ids, cu), lambda: adjust_logits(x.half(), ids, cu), lambda: adjust_logits(x.t(), ids, cu),
+        lambda: adjust_logits(x, ids, cu[:2]), lambda: adjust_logits(x, ids.cpu(), cu), lambda: adjust_logits(x, ids, cu, prompt_lens=lens[:1]),
+        lambda: adjust_logits(x, ids, None), lambda: adjust_logits(x, ids, cu, repetition=dev(np.ones(1, np.float32))),
+        lambda: adjust_logits(x, ids, cu, frequency=torch.ones(2, dtype=torch.float64, device="cuda")),
+        lambda: adjust_logits(x, ids, cu, bias=(cu, ids, dev(np.ones(4, np.float32)))), lambda: adjust_logits(x, ids, cu, mask=i32([[1]])),
+        lambda: adjust_logits(x, ids, cu, mask=i32([[1, 1]])), lambda: adjust_logits(x, ids, cu, mask=i32([[1, 1]]), mask_rows=s[:1]),
+        lambda: adjust_logits(x, ids, cu, out=x[:1]), lambda: adjust_logits(x[:1].expand(2, 50), ids, cu), lambda: adjust_logits(x.bfloat16(), ids, cu, out=x.bfloat16()),
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(E.ElisError):
+            call()
+            pytest.fail(f"call {i} was served")
+    assert pool.status() == (E.ELIS_OK, 0) and cache.status() == (E.ELIS_OK, 0) and int(pool.held.sum()) == 0
+
+
 def test_cache_past_four_gib():
     """Records whose places pass 32 bits: append, read and attention on the last pages of a large cache."""
     rng = np.random.default_rng(4)
