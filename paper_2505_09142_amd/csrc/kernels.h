@@ -188,6 +188,7 @@ hipError_t launch_kv_read(KvCacheView c, const int32_t* map, int n, uint16_t* k,
 // chunks of small_chunk keys, longer ones in tiles of 16 many_nb rows.
 struct KvAttnPlan {
     int small, small_nb, small_rows, small_chunk, small_chunks;
+    bool once;  // of those, records loaded past the caches
     bool many;
     int many_nb, many_tiles, many_chunk, many_chunks;
     long long small_most, many_most;  // chunks at most, with any window

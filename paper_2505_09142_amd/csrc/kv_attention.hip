@@ -194,8 +194,8 @@ struct Shared {
 };
 
 // One work-group's part, number `unit`. MANY: rows of every request with more than `small` rows, in tiles; else the
-// others, one tile each.
-template <int D, int NB, bool MANY>
+// others, one tile each, whose records nobody else reads: ONCE loads them past the caches.
+template <int D, int NB, bool MANY, bool ONCE>
 __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Shared<D, NB>& sh) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using R = Rec<D>;
@@ -203,6 +203,7 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
     constexpr int KS = D / 32;   // k-steps of the first product
     constexpr int DB = D / 16;   // 16-row blocks of O^T; values of a column
     constexpr bool QLDS = Shared<D, NB>::kQueries;
+    constexpr int kPolicy = ONCE ? 2 : 0;  // non-temporal
     auto& so = sh.o;
     auto& sm = sh.m;
     auto& sl = sh.l;
@@ -284,14 +285,14 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
         uint32_t ks[2], vs[2];
     };
     auto load_k = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
-        if constexpr (D == 128) x.k[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lk, 0, 0);
-        else x.k[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lk, 0, 0);
-        x.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lks & ~3u, 0, 0);
+        if constexpr (D == 128) x.k[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lk, 0, kPolicy);
+        else x.k[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lk, 0, kPolicy);
+        x.ks[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lks & ~3u, 0, kPolicy);
     };
     auto load_v = [&](__amdgpu_buffer_rsrc_t rec, Step& x, int u) {
-        if constexpr (D == 128) x.v[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lv, 0, 0);
-        else x.v[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lv, 0, 0);
-        x.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lvs, 0, 0);
+        if constexpr (D == 128) x.v[u] = __builtin_amdgcn_raw_buffer_load_b128(rec, lv, 0, kPolicy);
+        else x.v[u] = __builtin_amdgcn_raw_buffer_load_b64(rec, lv, 0, kPolicy);
+        x.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(rec, lvs, 0, kPolicy);
     };
     auto load = [&](int st, Step& x) {
 #pragma unroll
@@ -612,15 +613,15 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
 
 constexpr int waves_per_simd(int nb) { return nb == 1 ? 4 : nb == 2 ? 3 : 2; }
 
-template <int D, int NB, bool MANY>
+template <int D, int NB, bool MANY, bool ONCE>
 __global__ __launch_bounds__(kThreads, waves_per_simd(NB)) void kv_attention_kernel(KvAttnArgs a) {
     __shared__ __attribute__((aligned(16))) Shared<D, NB> sh;
-    attend<D, NB, MANY>(a, blockIdx.x, sh);
+    attend<D, NB, MANY, ONCE>(a, blockIdx.x, sh);
 }
 
 // Both at once: neither waits for the other's last work-groups. The long requests' tiles come first, the single tokens fill
 // in behind (two prompts of up to 512 tokens beside 30 tokens: 37 us, the tokens among the tiles 43, before them 42).
-template <int D, int NB, int NBM>
+template <int D, int NB, int NBM, bool ONCE>
 __global__ __launch_bounds__(kThreads, waves_per_simd(NBM)) void kv_attention_mixed_kernel(KvAttnArgs a, KvAttnMany m) {
     union Both {
         Shared<D, NBM> many;
@@ -629,9 +630,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(NBM)) void kv_attention_mi
     __shared__ __attribute__((aligned(16))) char raw[sizeof(Both)];
     Both& sh = *reinterpret_cast<Both*>(raw);
     if (blockIdx.x < static_cast<unsigned>(m.units)) {
-        attend<D, NBM, true>(m.of(a, D), blockIdx.x, sh.many);
+        attend<D, NBM, true, false>(m.of(a, D), blockIdx.x, sh.many);
     } else {
-        attend<D, NB, false>(a, blockIdx.x - m.units, sh.small);
+        attend<D, NB, false, ONCE>(a, blockIdx.x - m.units, sh.small);
     }
 }
 
@@ -732,15 +733,20 @@ hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
     const unsigned heads = static_cast<unsigned>(a.c.n_kv_heads);
     const unsigned small = p.small_rows > 0 ? heads * a.n * p.small_chunks : 0, many = heads * p.many_tiles * p.many_chunks;
     const KvAttnMany m{static_cast<int>(many), p.many_chunk, p.many_chunks, 16 * p.many_nb, p.small_parts};  // both may have chunk results at once
-    if (small && many) {
-        const auto f = p.small_nb == 2 ? (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 2, kNbMost<D>> : kv_attention_mixed_kernel<D, 2, 2>)
-                                       : (p.many_nb == 4 ? kv_attention_mixed_kernel<D, 1, kNbMost<D>> : kv_attention_mixed_kernel<D, 1, 2>);
-        ELIS_TRY(launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, m));
-    } else if (small) {
-        const auto f = p.small_nb == 1 ? kv_attention_kernel<D, 1, false> : kv_attention_kernel<D, 2, false>;
-        ELIS_TRY(launch_kernel(f, dim3(small), dim3(kThreads), 0, st, a));
+    if (small) {
+        const auto go = [&](auto nb, auto once) {
+            constexpr int NB = decltype(nb)::value;
+            constexpr bool ONCE = decltype(once)::value;
+            if (!many) return launch_kernel(kv_attention_kernel<D, NB, false, ONCE>, dim3(small), dim3(kThreads), 0, st, a);
+            const auto f = p.many_nb == 4 ? kv_attention_mixed_kernel<D, NB, kNbMost<D>, ONCE> : kv_attention_mixed_kernel<D, NB, 2, ONCE>;
+            return launch_kernel(f, dim3(small + many), dim3(kThreads), 0, st, a, m);
+        };
+        const std::integral_constant<int, 1> one{};
+        const std::integral_constant<int, 2> two{};
+        ELIS_TRY(p.once ? (p.small_nb == 1 ? go(one, std::true_type{}) : go(two, std::true_type{}))
+                        : (p.small_nb == 1 ? go(one, std::false_type{}) : go(two, std::false_type{})));
     } else if (many) {
-        const auto f = p.many_nb == 2 ? kv_attention_kernel<D, 2, true> : kv_attention_kernel<D, kNbMost<D>, true>;
+        const auto f = p.many_nb == 4 ? kv_attention_kernel<D, kNbMost<D>, true, false> : kv_attention_kernel<D, 2, true, false>;
         ELIS_TRY(launch_kernel(f, dim3(many), dim3(kThreads), 0, st, m.of(a, D)));
     }
     const long long small_joins = small && p.small_chunks > 1 ? static_cast<long long>(heads) * a.n * p.small_rows : 0;
@@ -755,6 +761,12 @@ hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
 long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
 }  // namespace
+
+// Short requests: records at most, from which on they are loaded past the caches. Nobody reads them again in a call, and in
+// the next one only what the memory-side cache of 256 MB holds is worth finding there (jobs, their median and longest length,
+// 8 kv heads of 128, through and past the caches: 48 of 16,000, 32,768 206 and 183 us; 128 of 1,500, 4,096 63 and 57.5; 90 of
+// 1,200, 4,300 38.9 and 35.3; but 32 of 2,000, 4,096 25.2 and 26.8; 64 of 900, 3,872 23.3 and 23.9).
+constexpr double kOnceBytes = 320 << 20;
 
 // Short requests: chunks. A work-group needs about 4.5 us whatever its keys and 0.5 us for each 128, and joining costs 4
 // us, so up to 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001
@@ -807,6 +819,7 @@ KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_he
     } else {
         p.many = true;
     }
+    p.once = static_cast<double>(n) * keys * n_kv_heads * 17 / 16 * d_head > kOnceBytes;
     p.many_chunks = 1;
     if (p.many) {
         const long long rows = static_cast<long long>(total_q) * group, longer = rows / (p.small + 1);

@@ -15,9 +15,10 @@ namespace elis {
 
 namespace {
 
-// 128 rows of 250,002 fp32 logits, 32 of 30,522 bf16: 512 threads and 4,096 tokens 63 / 6.6 us, 512 and 8,192 74 / 8.7,
-// 1,024 and 8,192 61 / 7.7, 256 and 4,096 80 / 7.9, 512 and 2,048 87 / 6.0 (without the early loads, and with the biases
-// added to the written output, 105 / 8.5). 63 us are 4.1 TB/s; a copy of 4 GiB runs at 4.7.
+// 128 rows of 250,002 fp32 logits, 32 of 30,522 bf16: 512 threads and 4,096 tokens 62 / 5.9 us, 512 and 8,192 70 / 7.1,
+// 1,024 and 8,192 60 / 6.4, 256 and 4,096 78 / 7.5, 512 and 2,048 88 / 5.9 (without the early loads, and with the biases
+// added to the written output, 105 / 8.5). Loads and stores past the
+// L2, since nothing here is read again, 57.5 / 6.0 (only the stores 62 / 5.9, neither 69.6 / 5.9): 4.5 TB/s; a copy of 4 GiB runs at 4.7.
 constexpr int kThreads = 512;
 constexpr int kChunk = 4096;          // tokens of a work-group
 constexpr int kVecs = kChunk / (4 * kThreads);  // groups of four a thread
@@ -34,11 +35,11 @@ __device__ __forceinline__ float load1(const void* p, long long i) {
 template <bool BF16>
 __device__ __forceinline__ f32x4 load4(const void* p, long long i) {
     if constexpr (BF16) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + i);
+        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + i));
         return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16),
                      __uint_as_float(w[1] & 0xFFFF0000u)};
     }
-    return *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i));
 }
 
 template <bool BF16>

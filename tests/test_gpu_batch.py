@@ -444,6 +444,23 @@ def test_wrappers_refuse_what_does_not_fit():
     assert pool.status() == (E.ELIS_OK, 0) and cache.status() == (E.ELIS_OK, 0) and int(pool.held.sum()) == 0
 
 
+@pytest.mark.parametrize("heads,kv_heads,d", [(8, 8, 128), (40, 2, 128), (12, 12, 64), (20, 1, 64)])
+@pytest.mark.parametrize("q_lens", [[1] * 6, [1, 60, 1, 0, 2, 1]])
+def test_attention_of_batches_that_may_be_long(heads, kv_heads, d, q_lens):
+    """Bounds on the lengths by which the batch may hold more than the caches."""
+    rng = np.random.default_rng(d + heads)
+    kv_lens = [700, 130, 1, 64, 300, 2500]
+    width = -(-420_000_000 // (6 * kv_heads * 17 * d // 16 * 128))
+    note(f"kv attention q={q_lens} heads={heads}/{kv_heads} d={d} of up to {width * 128} keys")
+    cache, blocks, k, v, _ = paged(rng, kv_lens, kv_heads, d, 128)
+    table = np.full((6, width), -1)
+    table[:, :blocks.shape[1]] = blocks
+    q = torch.from_numpy(rng.standard_normal((sum(q_lens), heads, d))).to("cuda").to(BF)
+    out = cache.attention(q, i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens), i32(table), max(q_lens), width * 128)
+    assert cache.status() == (E.ELIS_OK, 0)
+    check_attention(out, q, q_lens, kv_lens, k, v, d ** -0.5)
+
+
 def test_cache_past_four_gib():
     """Records whose places pass 32 bits: append, read and attention on the last pages of a large cache."""
     rng = np.random.default_rng(4)
