@@ -6,7 +6,6 @@ kernels, reached through the same-named calls of ``_elis``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import numpy as np
@@ -24,8 +23,13 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _torch_stream(stream) -> torch.cuda.Stream:
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An empty tensor that work on `stream` may write at once: memory that other streams' work may still use is not handed
+    out again to this one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _to_dev(a: np.ndarray, device) -> torch.Tensor:
@@ -245,13 +249,13 @@ class PagePool:
             raise E.ElisError(E.ELIS_EINVAL, "PagePool")
         made = tensors is None
         if made:
-            tensors = [torch.empty(s, dtype=torch.int32, device=device) for s in sizes]
+            tensors = [_empty(s, I32, device, stream) for s in sizes]
         for t, s in zip(tensors, sizes, strict=True):
             if tuple(t.shape) != s:
                 raise E.ElisError(E.ELIS_ESHAPE, "PagePool")
             _arg(t, torch.int32, tensors[0].get_device(), "PagePool")
         self.state, self.free_pages, self.held, self.table = tensors
-        self.scratch = torch.empty(4 * max_jobs + 4, dtype=torch.int32, device=self.state.device)
+        self.scratch = _empty(4 * max_jobs + 4, I32, self.state.device, stream)
         self.p = E.elis_page_pool(*(t.data_ptr() for t in (*tensors, self.scratch)), n_pages, page_tokens, max_jobs,
                                   max_pages)
         if made:
@@ -277,7 +281,7 @@ class PagePool:
         n, dev, where = slots.numel(), self.state.get_device(), "elis_pages_trim"
         if dev != _dev():
             raise E.ElisError(E.ELIS_EINVAL, where)
-        E.check(E.elis_pages_trim(self.p, _arg(slots, torch.int32, dev, where), _arg(lens, torch.int32, dev, where, n), n,
+        E.check(E.elis_pages_trim(self.p, _arg(slots, I32, dev, where), _arg(lens, I32, dev, where, n), n,
                                   _stream(stream)), where)
 
     def status(self, stream=None):
@@ -296,7 +300,7 @@ class KVCache:
         self.n_pages, self.page_tokens, self.n_kv_heads, self.d_head = n_pages, page_tokens, n_kv_heads, d_head
         made = buf is None
         if made:
-            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+            buf = _empty(nbytes + 256, torch.uint8, device, stream)
         base = (buf.data_ptr() + 255) // 256 * 256
         _arg(buf, torch.uint8, buf.get_device(), "KVCache", base - buf.data_ptr() + nbytes)
         self.buf, self.dev = buf, buf.get_device()
@@ -319,7 +323,7 @@ class KVCache:
         dev = self._here(where)
         ks = _heads(k, n, self.n_kv_heads, self.d_head, dev, where)
         vs = _heads(v, n, self.n_kv_heads, self.d_head, dev, where)
-        E.check(E.elis_kv_append(self.c, k.data_ptr(), v.data_ptr(), ks, vs, _arg(slot_map, torch.int32, dev, where), n,
+        E.check(E.elis_kv_append(self.c, k.data_ptr(), v.data_ptr(), ks, vs, _arg(slot_map, I32, dev, where), n,
                                  _stream(stream)), where)
 
     def read(self, slot_map: torch.Tensor, out_k: torch.Tensor, out_v: torch.Tensor, stream=None):
@@ -328,7 +332,7 @@ class KVCache:
         dev = self._here(where)
         ks = _heads(out_k, n, self.n_kv_heads, self.d_head, dev, where)
         vs = _heads(out_v, n, self.n_kv_heads, self.d_head, dev, where)
-        E.check(E.elis_kv_read(self.c, _arg(slot_map, torch.int32, dev, where), n, out_k.data_ptr(), out_v.data_ptr(), ks, vs,
+        E.check(E.elis_kv_read(self.c, _arg(slot_map, I32, dev, where), n, out_k.data_ptr(), out_v.data_ptr(), ks, vs,
                                _stream(stream)), where)
 
     def attention(self, q: torch.Tensor, cu_q: torch.Tensor, kv_lens: torch.Tensor, blocks: torch.Tensor, max_q: int,
@@ -343,7 +347,7 @@ class KVCache:
         total, heads, _ = q.shape
         d = self.d_head
         if out is None:
-            out = torch.empty((total, heads, d), dtype=torch.bfloat16, device=q.device)
+            out = _empty((total, heads, d), BF16, q.device, stream)
         qs, os_ = _heads(q, total, heads, d, dev, where), _heads(out, total, heads, d, dev, where)
         block_rows, block_cols = blocks.shape
         sizes = (n, total, max_q, max_kv, heads)
@@ -353,8 +357,7 @@ class KVCache:
         # nothing (256 bytes, not touched).
         ws, wsb = self._no_ws, self._need
         if wsb > 256:
-            with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream)):
-                scratch = torch.empty(wsb + 256, dtype=torch.uint8, device=q.device)
+            scratch = _empty(wsb + 256, torch.uint8, q.device, stream)
             ws = (scratch.data_ptr() + 255) // 256 * 256
         E.check(E.elis_kv_attention(self.c, q.data_ptr(), qs, _arg(cu_q, i32, dev, where, n + 1), n, total, max_q,
                                     _arg(blocks, i32, dev, where), block_rows, block_cols,
@@ -378,7 +381,7 @@ def adjust_logits(logits: torch.Tensor, token_ids: torch.Tensor | None, cu_seqle
         raise E.ElisError(E.ELIS_EINVAL, where)
     n, vocab = logits.shape
     if out is None:
-        out = torch.empty((n, vocab), dtype=torch.float32, device=logits.device)
+        out = _empty((n, vocab), F32, logits.device, stream)
     if out.shape != logits.shape or out.dtype is not F32 or out.stride(1) != 1 or out.get_device() != dev:
         raise E.ElisError(E.ELIS_EINVAL, where)
     f32, i32 = F32, I32
