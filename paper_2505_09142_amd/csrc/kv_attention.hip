@@ -647,22 +647,40 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
     const int wi = wid % WAVES;
     const bool many = w >= small_units;
     const int tile = many ? m.tile : small_tile;
-    int req, h, r;
+    int req = 0, h = 0, r = 0, tok = 0, head = 0;
     if (many) {
         w -= small_units;
         a = m.of(a, D);
-        const long long tok = w / a.n_heads;
-        if (tok >= a.total_q) return;
-        const int head = static_cast<int>(w - tok * a.n_heads);
-        req = find_segment(a.cu, a.n, static_cast<int>(tok));
-        h = head / a.group;
-        r = static_cast<int>(tok - a.cu[req]) * a.group + (head - h * a.group);
+        if (w / a.n_heads >= a.total_q) return;
+        tok = static_cast<int>(w / a.n_heads);
+        head = static_cast<int>(w - static_cast<long long>(tok) * a.n_heads);
     } else {
         r = static_cast<int>(w % a.small_rows);
         const long long u = w / a.small_rows;
         h = static_cast<int>(u % a.c.n_kv_heads);
         if (u / a.c.n_kv_heads >= a.n) return;
         req = static_cast<int>(u / a.c.n_kv_heads);
+    }
+    // Where the results are does not depend on the lengths: the first are requested along with them (one request of 30,001
+    // tokens 13.8 -> 13.0 us).
+    const size_t at = part_row(a, many, req, h, tok, head, r) * a.nchunks;
+    constexpr int PL = D / kWave;  // values a lane
+    constexpr int AHEAD = 8;       // chunks a wave fetches at a time, the first before their weights are known
+    typedef float fvec __attribute__((ext_vector_type(PL)));
+    fvec v[AHEAD];
+    auto fetch = [&](int i0, int last) {
+#pragma unroll
+        for (int y = 0; y < AHEAD; ++y) {
+            const int i = i0 + y * WAVES;
+            v[y] = *reinterpret_cast<const fvec*>(a.part_o + (at + (i < last ? i : last)) * D + lane * PL);
+        }
+    };
+    float2 ml = a.part_ml[at + (lane < a.nchunks ? lane : 0)];
+    fetch(wi, a.nchunks - 1);
+    if (many) {
+        req = find_segment(a.cu, a.n, tok);
+        h = head / a.group;
+        r = (tok - a.cu[req]) * a.group + (head - h * a.group);
     }
     const Request rq = request_of(a, req);
     const int rows = rq.ql * a.group;
@@ -672,33 +690,22 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
     span_of(a, rq, r0, r1, &lo, &hi);
     const int nc = chunks_of(lo, hi, a.chunk);
     if (nc == 1) return;  // every return is the same for the waves of a row
-    const int t = r / a.group, head = h * a.group + (r - t * a.group);
-    const size_t at = part_row(a, many, req, h, rq.q0 + t, head, r) * a.nchunks;
-    constexpr int PL = D / kWave;  // values a lane
-    constexpr int AHEAD = 8;       // chunks a wave fetches at a time, the first before their weights are known
-    typedef float fvec __attribute__((ext_vector_type(PL)));
     float top = kLowest, total = 0.f;
     fvec acc = 0.f;
     for (int base = 0; base < nc; base += kWave) {
         const int n = nc - base < kWave ? nc - base : kWave;
-        const float2 ml = lane < n ? a.part_ml[at + base + lane] : float2{kLowest, 0.f};
-        const float* p = a.part_o + (at + base) * D + lane * PL;
-        fvec v[AHEAD];
-        auto fetch = [&](int i0) {
-#pragma unroll
-            for (int y = 0; y < AHEAD; ++y) {
-                const int i = i0 + y * WAVES;
-                v[y] = *reinterpret_cast<const fvec*>(p + (i < n ? i : n - 1) * D);
-            }
-        };
-        fetch(wi);
+        if (base) {
+            ml = a.part_ml[at + base + (lane < n ? lane : 0)];
+            fetch(base + wi, base + n - 1);
+        }
+        if (lane >= n) ml = float2{kLowest, 0.f};
         const float mt = fmaxf(top, wave_max(ml.x));
         const float old = __builtin_amdgcn_exp2f(top - mt), wt = __builtin_amdgcn_exp2f(ml.x - mt);
         total = total * old + wave_sum(ml.y * wt);
         acc *= old;
         top = mt;
         for (int i0 = wi; i0 < n; i0 += AHEAD * WAVES) {
-            if (i0 > wi) fetch(i0);
+            if (i0 > wi) fetch(base + i0, base + n - 1);
 #pragma unroll
             for (int y = 0; y < AHEAD; ++y) {
                 const int i = i0 + y * WAVES;
@@ -717,7 +724,8 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
             for (int e = 0; e < PL; ++e) acc[e] += part[wid + x][lane * PL + e];
     }
     const float inv = total == 0.f ? 1.0f : 1.0f / total;
-    uint16_t* p = a.out + static_cast<long long>(rq.q0 + t) * a.out_stride + static_cast<long long>(head) * D + lane * PL;
+    const int t = r / a.group;
+    uint16_t* p = a.out + static_cast<long long>(rq.q0 + t) * a.out_stride + static_cast<long long>(h * a.group + (r - t * a.group)) * D + lane * PL;
 #pragma unroll
     for (int e = 0; e < PL; ++e) p[e] = f32_to_bf16(acc[e] * inv);
 }
