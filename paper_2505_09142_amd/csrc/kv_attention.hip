@@ -778,7 +778,7 @@ constexpr double kOnceBytes = 320 << 20;
 
 // Short requests: chunks. A work-group needs about 4.5 us whatever its keys and 0.5 us for each 128, and joining costs 4
 // us, so up to 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001
-// tokens and 8 kv heads: chunks of 512 / 1,024 / 2,048 keys 16.9 / 15.4 / 19.0 us), and at least three to a request that is
+// tokens and 8 kv heads: chunks of 512 / 640 / 1,024 / 1,280 keys 14.3 / 14.9 / 13.4 / 14.1 us), and at least three to a request that is
 // as long as max_kv, because the others are shorter (one chunk, three and six of them: 64 requests of up to 3,872 tokens
 // 23.9 / 23.1 / 24.1, 90 of up to 9,000 44.8 / 38.8 / 39.3, but 64 of up to 1,900 with 12 heads of 64 15.3 / 18.6 / 20.0: the
 // join), but not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 /
