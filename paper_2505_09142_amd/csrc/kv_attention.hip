@@ -25,9 +25,9 @@
 // makes NaN of exactly the rows that see it (where every row sees a record, its NaN goes through the products).
 //
 // Bounds. Single tokens: memory, 17/16 D bytes a key and kv head, once (48 requests of 16,000 tokens and 8 kv heads of 128:
-// 207 us, 5.0 TB/s, more than a copy reaches). Long prompts: the vector unit, which unpacks and takes exponentials beside
-// the products (2,048 tokens of 32 heads over 16,000 keys: 484 us, 1.04 PFLOP/s; vector unit busy 65 % of it, matrix unit
-// 41 %; they overlap little: two waves' 64 products and 232 vector instructions each take 1.7 us where either kind alone
+// 183 us, 5.7 TB/s). Long prompts: the vector unit, which unpacks and takes exponentials beside
+// the products (2,048 tokens of 32 heads over 16,000 keys: 480 us, 1.05 PFLOP/s; vector unit busy 61 % of it, matrix unit
+// 42 %; they overlap little: two waves' 64 products and 232 vector instructions each take 1.7 us where either kind alone
 // takes 0.9 and 1.1, and the kernel's 64 and 270 take 2.0). One request alone: latency. Its keys are split (chunks) and joined by a second launch.
 #include <math.h>
 
@@ -675,8 +675,13 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
             v[y] = *reinterpret_cast<const fvec*>(a.part_o + (at + (i < last ? i : last)) * D + lane * PL);
         }
     };
-    float2 ml = a.part_ml[at + (lane < a.nchunks ? lane : 0)];
-    fetch(wi, a.nchunks - 1);
+    float2 ml{};
+    auto begin = [&] {
+        ml = a.part_ml[at + (lane < a.nchunks ? lane : 0)];
+        fetch(wi, a.nchunks - 1);
+    };
+    const bool early = many || r < a.group;  // rows that a single token has
+    if (early) begin();
     if (many) {
         req = find_segment(a.cu, a.n, tok);
         h = head / a.group;
@@ -690,6 +695,7 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
     span_of(a, rq, r0, r1, &lo, &hi);
     const int nc = chunks_of(lo, hi, a.chunk);
     if (nc == 1) return;  // every return is the same for the waves of a row
+    if (!early) begin();
     float top = kLowest, total = 0.f;
     fvec acc = 0.f;
     for (int base = 0; base < nc; base += kWave) {
