@@ -413,7 +413,7 @@ def test_wrappers_refuse_what_does_not_fit():
     s, cu, m = i32([0, 1]), i32([0, 3, 5]), i32([0] * 5)
     kv, q = torch.zeros((5, 2, 64), dtype=BF, device="cuda"), torch.zeros((5, 4, 64), dtype=BF, device="cuda")
     lens, blocks = i32([3, 2]), i32([[0], [1]])
-    x, ids = torch.zeros((2, 50), device="cuda"), i32([1, 2, 3, 4, 5])
+    x, ids = torch.zeros((2, 50), dtype=torch.float32, device="cuda"), i32([1, 2, 3, 4, 5])
     calls = [
         lambda: pool.grow(s.cpu(), lens, cu, 5, m), lambda: pool.grow(s.long(), lens, cu, 5, m), lambda: pool.grow(s, lens[:1], cu, 5, m),
         lambda: pool.grow(s, lens, cu[:2], 5, m), lambda: pool.grow(s, lens, cu, 6, m), lambda: pool.grow(s, lens, cu, 5, m, out_blocks=blocks[:1]),
@@ -586,7 +586,7 @@ def test_logits(n, vocab, hist, pad, dtype):
     rows = rng.integers(-1, 4, n)
     f32 = lambda a: dev(np.asarray(a, np.float32))  # noqa: E731
     bias = (i32(b_cu), i32(b_tok), f32(b_val)) if len(b_tok) else None
-    full = torch.full((n + 1, vocab + 3), 77.0, device="cuda")
+    full = torch.full((n + 1, vocab + 3), 77.0, dtype=torch.float32, device="cuda")
     out = full[:n, 3:]
     for use_mask, use_rest in ((True, True), (False, True), (False, False)):
         kw = dict(repetition=f32(rep), frequency=f32(freq), presence=f32(pres), bias=bias, prompt_lens=i32(prompt)) if use_rest else {}
@@ -736,7 +736,7 @@ def test_captured_step(q_lens, kv_lens):
     smap = torch.zeros(T, dtype=torch.int32, device="cuda")
     blocks = torch.zeros((n, 400), dtype=torch.int32, device="cuda")
     q, k, v = (torch.zeros((T, h, d), dtype=BF, device="cuda") for h in (heads, kv_heads, kv_heads))
-    logits, ids, hcu = torch.zeros((n, vocab), device="cuda"), i32(rng.integers(0, vocab, 90)), i32([0, 10, 50, 90])
+    logits, ids, hcu = torch.zeros((n, vocab), dtype=torch.float32, device="cuda"), i32(rng.integers(0, vocab, 90)), i32([0, 10, 50, 90])
     o, y = torch.zeros_like(q), torch.zeros_like(logits)
     rep = dev(np.full(n, 1.3, np.float32))
     stream = torch.cuda.Stream()
@@ -766,7 +766,7 @@ def test_captured_step(q_lens, kv_lens):
         graph.replay()
         torch.cuda.synchronize()
         got = (o.clone(), y.clone(), smap.clone(), blocks.clone(), pool.state.clone())
-        (torch.randn(512, 512, device="cuda") @ torch.randn(512, 512, device="cuda")).sum().item()
+        torch.mm(*(torch.randn((512, 512), dtype=torch.float32, device="cuda") for _ in range(2))).sum().item()
         o2, y2 = torch.zeros_like(o), torch.zeros_like(y)
         step(o2, y2)
         torch.cuda.synchronize()

@@ -70,7 +70,7 @@ def test_slot_maps_and_logits_of_a_batch():
     assert slot_map.cpu().tolist() == want
     note("driver: logits with the table's histories")
     logits = torch.from_numpy(rng.standard_normal((4, vocab)).astype(np.float32)).cuda()
-    one = lambda v: torch.full((4,), v, device="cuda")  # noqa: E731
+    one = lambda v: torch.full((4,), v, dtype=torch.float32, device="cuda")  # noqa: E731
     out = drv.adjust_logits(jobs, logits, [len(prompts[j]) for j in jobs], repetition=one(1.5), frequency=one(0.25), presence=one(0.5))
     for i, j in enumerate(jobs):
         history = job_input(prompts[j], responses[j], gen[j], max_pos).tolist()
@@ -93,7 +93,7 @@ def test_batches_that_are_refused_or_empty():
     drv.start([1, 2], [0, 1])
     note("driver: empty and refused batches")
     drv.sync_tokens([1], {1: np.array([4, 5], dtype=np.int32)}, {1: np.zeros(0, np.int32)}, {1: 0})
-    logits = torch.zeros((2, 9), device="cuda")
+    logits = torch.zeros((2, 9), dtype=torch.float32, device="cuda")
     for jobs, prompts in (([1, 2], [2, 1]), ([1], [2]), ([1, 1], [2])):  # a job without tokens; rows or lengths that do not fit
         with pytest.raises(ValueError):
             drv.adjust_logits(jobs, logits, prompts)
