@@ -22,7 +22,9 @@ constexpr int kScan = 1024;   // threads of the scan
 constexpr int kEach = 2;      // entries a thread of it holds at a time (grow and trim of 200 entries: 1 / 2 / 4 of them 11.0 / 11.7 /
                               // 13.3 us, of 2,048: 21.1 / 20.0 / 22.1, of 20,000: 152 / 138 / 150)
 constexpr int kSmall = 128;   // entries up to which one launch does all,
-constexpr int kSmallWork = 32768;  // with at most so many cells and slots to write
+// with at most so many cells and slots to write. Grow and trim with the grow in one launch and in two, GPU's time / among other
+// calls: 12,900 of 64 jobs a step 9.7 / 10.0 and 9.2 / 13.0 us, 19,000 of 20 new jobs 20.2 / 20.1 and 11.1 / 13.1.
+constexpr int kSmallWork = 16384;
 constexpr int kFill = 256;    // threads of a work-group of the second launch
 constexpr int32_t kClaim = INT32_MIN;  // held[s] with its top bit set: named by an entry of the running call
 
@@ -128,13 +130,13 @@ __device__ __forceinline__ int block_scan(int v, int32_t* wave_tot, int* total) 
 template <bool GROW>
 __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
     __shared__ int32_t wave_tot[kScan / kWave];
-    __shared__ int32_t slot[kSmall], first[kSmall], h0s[kSmall], h1s[kSmall], lens[kSmall], cu[kSmall + 1], again[kSmall];
-    __shared__ int32_t taken_s;
+    __shared__ int32_t slot[kSmall], excl[kSmall], h0s[kSmall], h1s[kSmall], lens[kSmall], cu[kSmall + 1], again[kSmall];
+    __shared__ int32_t taken_s, more_s;
     __shared__ uint32_t bad_s;
     const int tid = threadIdx.x, i = tid;
     if (tid == 0) {
         bad_s = 0u;
-        taken_s = 0;
+        taken_s = more_s = 0;
     }
     const int count = clamp_count(a.p.state[1], a.p.n_pages);
     uint32_t bad = 0u;
@@ -187,6 +189,12 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
     }
     int total;
     const int incl = block_scan(move, wave_tot, &total);
+    const int top = (GROW ? count : count + total) - 1;  // stack place of the first page that moves
+    auto move_page = [&](int32_t of, int j, int at) {     // page j of job slot `of`
+        int32_t* cell = a.p.table + static_cast<size_t>(of) * a.p.max_pages + j;
+        if (GROW) *cell = a.p.free_pages[at];
+        else if (at >= 0 && at < a.p.n_pages) a.p.free_pages[at] = *cell;
+    };
     int h1 = h0;
     if (i < a.n) {
         if (GROW) {
@@ -194,13 +202,16 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
             if (!fits) bad |= ELIS_DEV_NO_PAGES;
             else h1 = h0 + move;
             if (total > count && move > 0 && fits) atomicMax(&taken_s, incl);
-            first[i] = count - 1 - (incl - move);
         } else {
             h1 = h0 - move;
-            first[i] = count + total - 1 - (incl - move);
         }
+        excl[i] = incl - move;
         h1s[i] = h1;
-        if (h1 != h0) a.p.held[s] = h1;
+        if (h1 != h0) {
+            a.p.held[s] = h1;
+            move_page(s, GROW ? h0 : h1, top - (incl - move));  // the only one, in a step of a token each
+            if (move > 1) more_s = 1;
+        }
     }
     if (bad) atomicOr(&bad_s, bad);
     __syncthreads();
@@ -210,15 +221,13 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
         if (bad_s) atomicOr(reinterpret_cast<uint32_t*>(&a.p.state[0]), bad_s);
     }
     auto page = [&](int k, int j) {  // of entry k, j < h1
-        return j < h0s[k] ? a.p.table[static_cast<size_t>(slot[k]) * a.p.max_pages + j] : a.p.free_pages[first[k] - (j - h0s[k])];
+        return j < h0s[k] ? a.p.table[static_cast<size_t>(slot[k]) * a.p.max_pages + j] : a.p.free_pages[top - excl[k] - (j - h0s[k])];
     };
-    for (int k = wid; k < a.n; k += kScan / kWave) {  // pages that move
-        const int p0 = GROW ? h0s[k] : h1s[k], p1 = GROW ? h1s[k] : h0s[k];
-        int32_t* row = p1 > p0 ? a.p.table + static_cast<size_t>(slot[k]) * a.p.max_pages : nullptr;
-        for (int j = p0 + lane; j < p1; j += kWave) {
-            const int at = first[k] - (j - p0);
-            if (GROW) row[j] = a.p.free_pages[at];
-            else if (at >= 0 && at < a.p.n_pages) a.p.free_pages[at] = row[j];
+    if (more_s) {  // the other pages that move, one a thread (a wave an entry took 4 us longer for 100 new requests)
+        for (int m = tid; m < total; m += kScan) {
+            const int k = find_segment(excl, a.n, m), j = (GROW ? h0s[k] : h1s[k]) + m - excl[k];
+            if (j >= (GROW ? h1s[k] : h0s[k])) break;  // entries that the free pages do not reach for, to the last
+            move_page(slot[k], j, top - m);
         }
     }
     if (GROW && a.blocks) {
@@ -236,7 +245,7 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
                 const int kc = in[u] ? k : 0, h0k = h0s[kc];
                 const bool has = in[u] && j < h1s[kc];
                 const int32_t* from = a.slots;
-                if (has) from = j < h0k ? a.p.table + static_cast<size_t>(slot[kc]) * a.p.max_pages + j : a.p.free_pages + (first[kc] - (j - h0k));
+                if (has) from = j < h0k ? a.p.table + static_cast<size_t>(slot[kc]) * a.p.max_pages + j : a.p.free_pages + (top - excl[kc] - (j - h0k));
                 v[u] = *from;
                 v[u] = has ? v[u] : -1;
                 k += dk;
