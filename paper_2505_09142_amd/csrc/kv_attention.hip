@@ -45,17 +45,11 @@ constexpr int kThreads = kWaves * kWave;
 constexpr float kLowest = -3.0e38f;  // a maximum over no keys: finite, so that differences of maxima are numbers
 constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
 
-// Maxima as single instructions: fmaxf first quiets each operand's signalling NaN with an instruction of its own.
-__device__ __forceinline__ float max2(float x, float y) {
-    float r;
-    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
-    return r;
-}
-__device__ __forceinline__ float max3(float x, float y, float z) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
-    return r;
-}
+// Maxima in single instructions, v_maximum3_f32: fmaxf first quiets each operand's signalling NaN with an instruction of its
+// own (56 more of them for a step of 64 rows). A NaN among the operands is the result. By builtins, because the compiler keeps
+// the wait states between a matrix product and the first reader of its result only where it knows that reader.
+__device__ __forceinline__ float max2(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+__device__ __forceinline__ float max3(float x, float y, float z) { return max2(max2(x, y), z); }
 
 // s + both halves of w, a pair of bf16.
 __device__ __forceinline__ float dot2(uint32_t w, float s) {
@@ -463,7 +457,7 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
                     if (j + 1 < NB) over = max3(over, x0, fmaf(t[(j + 1) % NB], sc, -m[(j + 1) % NB]));
                     else over = x0;
                 }
-                if (__ballot(over > 8.f) != 0ull) {
+                if (__ballot(!(over <= 8.f)) != 0ull) {  // a NaN too: it is one row's alone, and may hide another row's score
 #pragma unroll
                     for (int j = 0; j < NB; ++j) {
                         const float mn = max2(m[j], ceilf(quad_max(t[j]) * sc));
