@@ -6,6 +6,7 @@
 #include <tuple>
 
 #include "common.h"
+#include "kv_plan.h"
 
 namespace elis {
 
@@ -184,18 +185,6 @@ hipError_t launch_kv_append(KvCacheView c, const uint16_t* k, const uint16_t* v,
 hipError_t launch_kv_read(KvCacheView c, const int32_t* map, int n, uint16_t* k, uint16_t* v, long long k_stride, long long v_stride, hipStream_t st);
 
 // kv_attention.hip
-// Launches of one call: requests of up to `small` rows (new tokens x heads of a group) in one tile of 16 small_nb rows and
-// chunks of small_chunk keys, longer ones in tiles of 16 many_nb rows.
-struct KvAttnPlan {
-    int small, small_nb, small_rows, small_chunk, small_chunks;
-    bool once;  // of those, records loaded past the caches
-    bool many;
-    int many_nb, many_tiles, many_chunk, many_chunks;
-    long long small_most, many_most;  // chunks at most, with any window
-    size_t small_parts, many_parts;  // chunk results to join (d_head floats and two more each)
-};
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int d_head, int window);
-long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads);
 struct KvAttnArgs {
     KvCacheView c;
     const uint16_t* q;
@@ -229,11 +218,6 @@ struct KvAttnMany {
         return a;
     }
 };
-// Row of the chunk results that (request, kv head, row) or (token, head) has.
-__device__ __forceinline__ size_t part_row(const KvAttnArgs& a, bool many, int req, int h, int tok, int head, int r) {
-    return many ? static_cast<size_t>(tok) * a.n_heads + head
-                : (static_cast<size_t>(req) * a.c.n_kv_heads + h) * a.small_rows + r;
-}
 hipError_t launch_kv_attention(KvAttnArgs a, const KvAttnPlan& p, hipStream_t st);
 
 // logits.hip

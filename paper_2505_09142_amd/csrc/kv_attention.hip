@@ -594,7 +594,7 @@ __device__ __forceinline__ void attend(const KvAttnArgs& a, unsigned unit, Share
                     for (int e = 0; e < PT; ++e) p[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
                 }
             } else {
-                const size_t at = part_row(a, MANY, req, h, rq.q0 + t, head, r) * a.nchunks + chunk_i;
+                const size_t at = kv_part_row(MANY, req, h, rq.q0 + t, head, r, a.n_heads, a.c.n_kv_heads, a.small_rows) * a.nchunks + chunk_i;
                 float* p = a.part_o + at * D + jd;
 #pragma unroll
                 for (int e = 0; e < PT; e += 4) *reinterpret_cast<f32x4*>(p + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
@@ -632,32 +632,21 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(NBM)) void kv_attention_mi
 
 // Joins the chunks of split rows, in an order that depends on their number alone. WAVES waves a row, each taking every
 // WAVES-th chunk: with one wave a row of 118 chunks took 38 us, its loads one behind the other.
-// The first small_units rows are those of short requests (a.small_rows each), then comes one for each token and head.
+// A wave past the last row reads nothing: its place in the chunk results may lie behind them.
 template <int D, int WAVES>
-__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAttnMany m, long long small_units, int small_tile) {
+__global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAttnMany m, KvJoins joins, int small_tile) {
     __shared__ __attribute__((aligned(16))) float part[WAVES > 1 ? kWaves : 1][D];
     const int lane = threadIdx.x & (kWave - 1), wid = threadIdx.x / kWave;
-    long long w = static_cast<long long>(blockIdx.x) * (kWaves / WAVES) + wid / WAVES;
+    const KvJoinRow x = kv_join_row(static_cast<long long>(blockIdx.x) * (kWaves / WAVES) + wid / WAVES, joins, a.small_rows, a.n_heads, a.c.n_kv_heads);
+    if (!x.any) return;
     const int wi = wid % WAVES;
-    const bool many = w >= small_units;
+    const bool many = x.many;
     const int tile = many ? m.tile : small_tile;
-    int req = 0, h = 0, r = 0, tok = 0, head = 0;
-    if (many) {
-        w -= small_units;
-        a = m.of(a, D);
-        if (w / a.n_heads >= a.total_q) return;
-        tok = static_cast<int>(w / a.n_heads);
-        head = static_cast<int>(w - static_cast<long long>(tok) * a.n_heads);
-    } else {
-        r = static_cast<int>(w % a.small_rows);
-        const long long u = w / a.small_rows;
-        h = static_cast<int>(u % a.c.n_kv_heads);
-        if (u / a.c.n_kv_heads >= a.n) return;
-        req = static_cast<int>(u / a.c.n_kv_heads);
-    }
+    int req = x.req, h = x.h, r = x.r;
+    if (many) a = m.of(a, D);
     // Where the results are does not depend on the lengths: the first are requested along with them (one request of 30,001
     // tokens 13.8 -> 13.0 us).
-    const size_t at = part_row(a, many, req, h, tok, head, r) * a.nchunks;
+    const size_t at = kv_part_row(many, req, h, x.tok, x.head, r, a.n_heads, a.c.n_kv_heads, a.small_rows) * a.nchunks;
     constexpr int PL = D / kWave;  // values a lane
     constexpr int AHEAD = 8;       // chunks a wave fetches at a time, the first before their weights are known
     typedef float fvec __attribute__((ext_vector_type(PL)));
@@ -677,9 +666,9 @@ __global__ __launch_bounds__(kThreads) void kv_combine_kernel(KvAttnArgs a, KvAt
     const bool early = many || r < a.group;  // rows that a single token has
     if (early) begin();
     if (many) {
-        req = find_segment(a.cu, a.n, tok);
-        h = head / a.group;
-        r = (tok - a.cu[req]) * a.group + (head - h * a.group);
+        req = find_segment(a.cu, a.n, x.tok);
+        h = x.head / a.group;
+        r = (x.tok - a.cu[req]) * a.group + (x.head - h * a.group);
     }
     const Request rq = request_of(a, req);
     const int rows = rq.ql * a.group;
@@ -757,103 +746,14 @@ hipError_t run(const KvAttnArgs& args, const KvAttnPlan& p, hipStream_t st) {
         const auto f = p.many_nb == 4 ? kv_attention_kernel<D, kNbMost<D>, true, false> : kv_attention_kernel<D, 2, true, false>;
         ELIS_TRY(launch_kernel(f, dim3(many), dim3(kThreads), 0, st, m.of(a, D)));
     }
-    const long long small_joins = small && p.small_chunks > 1 ? static_cast<long long>(heads) * a.n * p.small_rows : 0;
-    const long long joins = small_joins + (many && p.many_chunks > 1 ? static_cast<long long>(a.total_q) * a.n_heads : 0);
-    if (joins == 0) return hipSuccess;
-    const bool wide = (small_joins ? p.small_chunks : 0) > 8 || (joins > small_joins && p.many_chunks > 8);
-    const auto f = wide ? kv_combine_kernel<D, kWaves> : kv_combine_kernel<D, 1>;
-    const unsigned grid = static_cast<unsigned>(wide ? joins : (joins + kWaves - 1) / kWaves);
-    return launch_kernel(f, dim3(grid), dim3(kThreads), 0, st, a, m, small_joins, 16 * p.small_nb);
+    const KvJoins joins = kv_joins(p, a.n, a.total_q, a.n_heads, a.c.n_kv_heads);
+    if (joins.all == 0) return hipSuccess;
+    const auto f = joins.wide ? kv_combine_kernel<D, kWaves> : kv_combine_kernel<D, 1>;
+    const unsigned grid = static_cast<unsigned>(joins.wide ? joins.all : (joins.all + kWaves - 1) / kWaves);
+    return launch_kernel(f, dim3(grid), dim3(kThreads), 0, st, a, m, joins, 16 * p.small_nb);
 }
-
-long long round_up(long long x, long long to) { return (x + to - 1) / to * to; }
 
 }  // namespace
-
-// Short requests: records at most, from which on they are loaded past the caches. Nobody reads them again in a call, and in
-// the next one only what the memory-side cache of 256 MB holds is worth finding there (jobs, their median and longest length,
-// 8 kv heads of 128, through and past the caches: 48 of 16,000, 32,768 206 and 183 us; 128 of 1,500, 4,096 63 and 57.5; 90 of
-// 1,200, 4,300 38.9 and 35.3; but 32 of 2,000, 4,096 25.2 and 26.8; 64 of 900, 3,872 23.3 and 23.9).
-constexpr double kOnceBytes = 320 << 20;
-
-// Short requests: chunks. A work-group needs about 4.5 us whatever its keys and 0.5 us for each 128, and joining costs 4
-// us, so up to 1,024 keys are not split. Beyond, there should be a work-group for each of 256 CUs (one request of 30,001
-// tokens and 8 kv heads: chunks of 512 / 640 / 1,024 / 1,280 keys 14.3 / 14.9 / 13.4 / 14.1 us), and at least three to a request that is
-// as long as max_kv, because the others are shorter (one chunk, three and six of them: 64 requests of up to 3,872 tokens
-// 23.9 / 23.1 / 24.1, 90 of up to 9,000 44.8 / 38.8 / 39.3, but 64 of up to 1,900 with 12 heads of 64 15.3 / 18.6 / 20.0: the
-// join), but not more than the fill of the machine asks for (48 requests of up to 32,768: 512 / 1,024 / 2,048 242 / 219 /
-// 206).
-//
-// Long requests: tiles of 32 rows, of which a CU runs three at a time, a 128-key round of theirs in 1.5 us; or, with heads
-// of 128, of 64 rows, two at a time in 2.05. What counts is how many fills of the 256 CUs they take, at 3 : 4 (tokens of 32
-// query and 8 kv heads over 9,000 keys: 512 tokens 32 rows 101 us, 64 rows 118; 1,000 165, 147; 1,500 227, 262; 2,048 290,
-// 265), if the tiles have about the same keys and single tokens do not fill the gaps (four prompts of 1,024 tokens with no
-// keys before them 63 and 67; prompts of up to 900 beside 8 tokens 168 and 182). They are split over the keys where they do
-// not fill the machine (two of 185 tokens of 20 heads over 2,676 keys 42 and 26 us; 100 tokens of 8 heads over 9,000: 62 and
-// 21); of more than 1,024 rows only up to half a fill, because joining costs more (of 8 heads over 9,000 keys, half and whole
-// fill: 200 tokens 30.5 and 29.0, 500 43.0 and 45.8).
-KvAttnPlan plan_kv_attention(int n, int total_q, int max_q, int max_kv, int n_heads, int n_kv_heads, int d_head, int window) {
-    KvAttnPlan p{};
-    const int group = n_heads / n_kv_heads;
-    const long long most = static_cast<long long>(max_q) * group;
-    // keys that a tile (at most 64 tokens) can see, on whole records
-    const long long reach = window > 0 && window < max_kv ? static_cast<long long>(window) + (max_q < 64 ? max_q : 64) + kRecTokens : max_kv;
-    const long long keys = reach < max_kv ? reach : max_kv;
-    // Chunks of the keys, about `want`; returns how many there can be for these sizes with any window: the workspace
-    // does not depend on it.
-    auto split = [&](long long want, long long least, long long largest, int* chunk, int* chunks) {
-        long long c = keys;
-        if (keys > 1024 && want > 1) {
-            c = round_up((keys + want - 1) / want, 128);
-            c = c < least ? least : c > largest ? largest : c;
-        }
-        *chunk = static_cast<int>(c < 1 ? 1 : round_up(c, 16));
-        *chunks = static_cast<int>(keys > *chunk ? (keys + *chunk - 1) / *chunk : 1);
-        if (max_kv <= 1024 || want <= 1) return 1LL;
-        const long long by_size = (max_kv + largest - 1) / largest;
-        return want > by_size ? want : by_size;
-    };
-    long long small_most = 1, many_most = 1;
-    // one tile of 16 or 32 rows holds a request, or (of longer ones) at least a single token
-    const long long fit = most <= 32 ? most : group;
-    if (fit <= 32) {
-        p.small_nb = fit <= 16 ? 1 : 2;
-        p.small = 16 * p.small_nb;
-        p.small_rows = static_cast<int>(most < p.small ? most : p.small);
-        p.many = most > p.small;
-        if (p.many && static_cast<long long>(n) * max_q == total_q) p.small = p.small_rows = 0;  // every request looks long
-        const long long per = static_cast<long long>(n) * n_kv_heads, want = (256 + per - 1) / per;
-        small_most = split(want < 3 ? 3 : want, 256, 2048, &p.small_chunk, &p.small_chunks);
-    } else {
-        p.many = true;
-    }
-    p.once = static_cast<double>(n) * keys * n_kv_heads * 17 / 16 * d_head > kOnceBytes;
-    p.many_chunks = 1;
-    if (p.many) {
-        const long long rows = static_cast<long long>(total_q) * group, longer = rows / (p.small + 1);
-        const long long t4 = (rows + 63) / 64 * n_kv_heads, t2 = (rows + 31) / 32 * n_kv_heads;
-        const bool alone = p.small_rows == 0 || 4LL * n * n_kv_heads * small_most <= t4, even = max_kv > 2LL * max_q;
-        p.many_nb = d_head == 128 && alone && even && 4 * ((t4 + 511) / 512) < 3 * ((t2 + 767) / 768) ? 4 : 2;
-        const int tile = 16 * p.many_nb;
-        p.many_tiles = static_cast<int>(rows / tile + (longer < n ? longer : n));  // at most: every long request's last tile cut
-        const long long per = (rows / tile + 1) * n_kv_heads;
-        const long long fill = rows <= 1024 ? 256 : 128;
-        many_most = split((fill + per - 1) / per, rows <= 1024 ? 512 : 1024, max_kv, &p.many_chunk, &p.many_chunks);
-    }
-    p.small_parts = p.small_rows > 0 && small_most > 1 ? static_cast<size_t>(n) * n_kv_heads * p.small_rows * small_most : 0;
-    p.many_parts = p.many && many_most > 1 ? static_cast<size_t>(total_q) * n_heads * many_most : 0;
-    p.small_most = small_most;
-    p.many_most = many_most;
-    return p;
-}
-
-// At most, with any window, work-groups of a launch (or rows to join: a work-group each).
-long long kv_attention_work_groups(const KvAttnPlan& p, int n, int n_kv_heads) {
-    const long long small = static_cast<long long>(n) * n_kv_heads;
-    const long long parts = small * p.small_most + static_cast<long long>(n_kv_heads) * p.many_tiles * p.many_most;
-    const long long joins = p.small_most > 1 ? small * p.small_rows : 0;  // rows of long requests are fewer where they are split
-    return parts > joins ? parts : joins;
-}
 
 hipError_t launch_kv_attention(KvAttnArgs a, const KvAttnPlan& p, hipStream_t st) {
     a.small = p.small;

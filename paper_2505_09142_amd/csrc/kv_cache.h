@@ -12,7 +12,6 @@
 
 namespace elis {
 
-constexpr int kRecTokens = 16;
 constexpr size_t kCacheHeader = 256;  // the status word
 
 template <int D>
