@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kScan) void pages_small_kernel(FillArgs a) {
         if (GROW && a.map) {
             o0 = a.cu[ic];
             o1 = a.cu[ic + 1];
-            cu[i] = o0;
+            if (i < a.n) cu[i] = o0;  // the place behind them is the last entry's alone
             if (i == a.n - 1) cu[a.n] = o1;
         }
         if (i >= a.n) {
