@@ -116,7 +116,9 @@ class DeviceRoundDriver:
     when it starts), packs the re-score set on the device, predicts, caches the
     predictions in the table, and selects over the cached predictions of the
     candidates; the chosen slots are the round's only device-to-host transfer.
-    Every upload of a call goes through one pinned staging buffer in one copy.
+    Every upload of a call goes through one pinned staging buffer in one copy. All calls
+    go to the current stream, which has to be the same for every call: buffers are used
+    again in its order.
 
     With ``pages`` (a PagePool with a slot for every job slot) a job's table slot is its
     slot of the pool too: reserve() gives the chosen jobs pages of the served model's KV
@@ -231,9 +233,11 @@ class DeviceRoundDriver:
         d_slots, d_lens = self._upload(self._slots(jobs), np.zeros(len(jobs), dtype=np.int32))
         self.pages.trim(d_slots, d_lens)
 
-    def adjust_logits(self, jobs, logits: torch.Tensor, prompt_lens, out: torch.Tensor | None = None, **kw) -> torch.Tensor:
+    def adjust_logits(self, jobs, logits: torch.Tensor, prompt_lens, out: torch.Tensor | None = None, *, repetition=None,
+                      frequency=None, presence=None, bias=None, mask=None, mask_rows=None) -> torch.Tensor:
         """device.adjust_logits on one row of logits a job, with the tokens that the table holds as its history (past
-        max_pos tokens the first one and the most recent max_pos - 1). The other arguments are passed on."""
+        max_pos tokens the first one and the most recent max_pos - 1). No stream is taken: the histories are packed, like
+        all of the driver's work, on the current one."""
         n = len(jobs)
         if logits.dim() != 2 or logits.shape[0] != n or len(prompt_lens) != n:
             raise ValueError("one row of logits and one prompt length for each job")
@@ -250,7 +254,8 @@ class DeviceRoundDriver:
         ids, cu = self._buffers(T, n)
         d_slots, d_seen = self._upload(self._slots(jobs), seen.astype(np.int32))
         self.table.pack(d_slots, T, int(held.max()), ids, cu)
-        return adjust_logits(logits, ids, cu, out, prompt_lens=d_seen, **kw)
+        return adjust_logits(logits, ids, cu, out, prompt_lens=d_seen, repetition=repetition, frequency=frequency,
+                             presence=presence, bias=bias, mask=mask, mask_rows=mask_rows)
 
     def _buffers(self, T: int, n: int):
         """Packed token ids and offsets of n jobs with T tokens (views of buffers that grow on demand)."""
