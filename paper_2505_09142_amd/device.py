@@ -312,7 +312,7 @@ class KVCache:
         self.c = E.elis_kv_cache(base, n_pages, page_tokens, n_kv_heads, d_head)
         self.ws = Workspace(buf.device)
         self._no_ws = self.ws.get(256)[0]
-        self._sizes, self._need = None, 0  # of the last attention call, and the workspace they take
+        self._last = None, 0  # sizes of an attention call and the workspace they take: one tuple, so that threads see a pair
         if made:
             _made_on(self.dev, "elis_kv_init")
             E.check(E.elis_kv_init(self.c, _stream(stream)), "elis_kv_init")
@@ -356,11 +356,12 @@ class KVCache:
         qs, os_ = _heads(q, total, heads, d, dev, where), _heads(out, total, heads, d, dev, where)
         block_rows, block_cols = blocks.shape
         sizes = (n, total, max_q, max_kv, heads)
-        if sizes != self._sizes:
-            self._need, self._sizes = E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d), sizes
+        last = self._last
+        if sizes != last[0]:
+            self._last = last = sizes, E.elis_kv_attention_workspace_bytes(*sizes, self.n_kv_heads, d)
         # A workspace of the call's own: calls on several streams, and captured graphs, share only the one that holds
         # nothing (256 bytes, not touched).
-        ws, wsb = self._no_ws, self._need
+        ws, wsb = self._no_ws, last[1]
         if wsb > 256:
             scratch = _empty(wsb + 256, torch.uint8, q.device, stream)
             ws = (scratch.data_ptr() + 255) // 256 * 256
