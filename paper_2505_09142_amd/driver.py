@@ -215,8 +215,9 @@ class DeviceRoundDriver:
     def reserve(self, jobs, lens, new=None, out_slot_map: torch.Tensor | None = None,
                 out_blocks: torch.Tensor | None = None) -> torch.Tensor:
         """Pages for the jobs' lens tokens, in the order of the call (the selection's: the first jobs are served first
-        when pages run out). With `new`, the last new[i] of job i's tokens are this step's: their cache slots go into
-        out_slot_map. Returns the jobs' slots, the rows of the pool's table, on the device (valid until the next call)."""
+        when pages run out; `pages.status()` tells that they did, `pages.held` who was served). With `new`, the last new[i]
+        of job i's tokens are this step's: their cache slots go into out_slot_map. Returns the jobs' slots, the rows of the
+        pool's table, on the device (valid until the next call)."""
         if len(lens) != len(jobs):
             raise ValueError("one length for each job")
         cu = np.zeros(len(jobs) + 1, dtype=np.int32)

@@ -25,10 +25,14 @@ Starvation control and preemption cost (Sec. 3.4 leaves both open):
                 the window waits for it.
 
 The round driver (DeviceRoundDriver or HostRoundDriver) owns the predictor,
-the key cache and the selection; the loop itself is host bookkeeping only. With
-a page pool (DeviceRoundDriver's `pages`) the chosen jobs hold the KV pages of
-their prompt and of the tokens they will have at the window's end; preempted and
-finished jobs give theirs back.
+the key cache and the selection; the loop itself is host bookkeeping only.
+
+With a page pool (DeviceRoundDriver's `pages`) the batch's jobs hold the KV pages
+of their prompt and of the tokens they will have at the window's end; preempted
+and finished jobs give theirs back. A job runs only with its pages: the batch is
+cut, from its last job on, to what the pages that were free at the start hold, and
+a job that is cut off is not chosen (so it is preempted if it ran before). A
+schedule with a job that the pool can never hold is refused.
 """
 from __future__ import annotations
 
@@ -36,6 +40,8 @@ import time
 from dataclasses import dataclass, field
 
 import numpy as np
+
+from . import _elis as E
 
 POLICIES = ("isrtf", "fcfs", "sjf")
 
@@ -64,6 +70,11 @@ class ScheduleResult:
     generated: np.ndarray = None
 
 
+def pages_of(lens, pages) -> np.ndarray:
+    """Pages that so many tokens take."""
+    return -(-np.asarray(lens, dtype=np.int64) // pages.page_tokens)
+
+
 def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cost: float, batch_cap: int,
                  policy: str = "isrtf", key_fn=None, rescore: str = "pool", end_rule: str = "all",
                  max_rounds: int | None = None, aging: float = 0.0, prefill_cost: float = 0.0) -> ScheduleResult:
@@ -83,7 +94,12 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
     last_batch: list = []
     next_arrival, finished, now = 0, 0, 0.0
     use_encoder = policy == "isrtf" and key_fn is None
-    pages = getattr(driver, "pages", None) is not None
+    pages = getattr(driver, "pages", None)
+    if pages is not None:
+        E.check(pages.status()[0], "run_schedule: the page pool")
+        room = int(pages.state[1])   # nobody else takes pages while the schedule runs (checked at its end)
+        if n and pages_of(plen + total, pages).max() > min(room, pages.max_pages):
+            raise ValueError("a job that the page pool cannot hold")
     out = ScheduleResult()
     while finished < n and (max_rounds is None or len(out.rounds) < max_rounds):
         fresh = []
@@ -120,6 +136,18 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
             driver.store_keys(rescore_set, keys)
         chosen = [int(j) for j in driver.select(candidates, batch_cap, wait=wait, aging=aging)]
         latency = time.perf_counter() - t0
+        while True:
+            budget = {j: int(min(window, total[j] - gen[j])) for j in chosen}
+            if end_rule == "all":
+                steps = max(budget.values())
+            elif end_rule == "first":
+                steps = min(budget.values())
+            else:
+                raise ValueError(end_rule)
+            lens = [int(plen[j] + gen[j]) + min(budget[j], steps) for j in chosen]
+            if pages is None or pages_of(lens, pages).sum() <= room:
+                break
+            chosen.pop()
         in_batch = set(chosen)
         gone = [j for j in last_batch if j not in in_batch]
         for j in gone:
@@ -128,16 +156,9 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
         resumed = sorted(j for j in chosen if dropped[j])
         prefill_s = prefill_cost * sum(int(plen[j] + gen[j]) for j in resumed) if resumed else 0.0
         dropped[resumed] = False
-        budget = {j: int(min(window, total[j] - gen[j])) for j in chosen}
-        if end_rule == "all":
-            steps = max(budget.values())
-        elif end_rule == "first":
-            steps = min(budget.values())
-        else:
-            raise ValueError(end_rule)
-        if pages:
+        if pages is not None:
             driver.drop(gone)
-            driver.reserve(chosen, [int(plen[j] + gen[j]) + min(budget[j], steps) for j in chosen])
+            driver.reserve(chosen, lens)
         end = now + prefill_s + steps * step_cost
         done_now = []
         last_batch = []
@@ -157,6 +178,8 @@ def run_schedule(arrival_t, prompts, responses, driver, *, window: int, step_cos
         out.rounds.append(Round(now, rescore_set, keys, candidates, chosen, steps, latency, wait, resumed,
                                 prefill_s))
         now = end
+    if pages is not None:
+        E.check(pages.status()[0], "run_schedule: the page pool")
     for r in out.rounds:
         if not isinstance(r.pred, np.ndarray):
             r.pred = r.pred.cpu().numpy()
