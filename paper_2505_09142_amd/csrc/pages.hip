@@ -26,6 +26,7 @@ constexpr int kSmall = 128;   // entries up to which one launch does all,
 // calls: 12,900 of 64 jobs a step 9.7 / 10.0 and 9.2 / 13.0 us, 19,000 of 20 new jobs 20.2 / 20.1 and 11.1 / 13.1.
 constexpr int kSmallWork = 16384;
 constexpr int kFill = 256;    // threads of a work-group of the second launch
+constexpr int kFillGroups = 65536;  // of them in a row of the grid: a row has fewer than 2^32 threads, a call up to 2^29 entries
 constexpr int32_t kClaim = INT32_MIN;  // held[s] with its top bit set: named by an entry of the running call
 
 struct FillArgs {
@@ -364,7 +365,8 @@ __global__ __launch_bounds__(kScan) void pages_scan_kernel(FillArgs a) {
 
 template <bool GROW>
 __global__ __launch_bounds__(kFill) void pages_fill_kernel(FillArgs a, int parts) {
-    const int i = blockIdx.x / parts, part = blockIdx.x - i * parts;
+    const int group = blockIdx.x / parts, part = blockIdx.x - group * parts, i = blockIdx.y * kFillGroups + group;
+    if (i >= a.n) return;
     const int32_t* e = a.p.scratch + 4 * static_cast<size_t>(i);
     const int first = e[0] + (GROW ? 0 : a.p.scratch[4 * static_cast<size_t>(a.p.max_jobs)]), h0 = e[1], h1 = e[2];
     const int32_t s = a.slots[i];
@@ -396,8 +398,10 @@ hipError_t launch_pages(const FillArgs& a, hipStream_t st) {
     // 15.8 / 15.9 / 15.9 / 19.2, 1,000 jobs a step 14.7 / 14.1 / 14.2 / 14.1).
     long long parts = work / (static_cast<long long>(a.n) * 2 * kFill);
     parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
-    if (parts * a.n > 65536) parts = 1;
-    return launch_kernel(pages_fill_kernel<GROW>, dim3(static_cast<unsigned>(parts * a.n)), dim3(kFill), 0, st, a, static_cast<int>(parts));
+    if (parts * a.n > kFillGroups) parts = 1;
+    const int row = a.n < kFillGroups ? a.n : kFillGroups;
+    return launch_kernel(pages_fill_kernel<GROW>, dim3(static_cast<unsigned>(parts * row), static_cast<unsigned>((a.n - 1) / kFillGroups + 1)), dim3(kFill), 0,
+                         st, a, static_cast<int>(parts));
 }
 
 }  // namespace

@@ -49,6 +49,8 @@ inline ucontext_t scheduler;
 inline unsigned current, order_seed;  // 0: ascending, 1: descending, else shuffled by the seed
 inline uint64_t wave_value[2048];
 inline int any_acc, any_result;
+inline bool dry;                   // launches are noted, not run
+inline unsigned long long most;    // threads in a row of the largest launch noted, 0 from a launch of too many rows on
 inline std::function<void()> body;
 
 inline void wait(State s) {
@@ -176,6 +178,11 @@ namespace elis {
 
 template <typename... P, typename... A>
 inline hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t, hipStream_t, A... a) {
+    if (simt::dry) {
+        const unsigned long long row = static_cast<unsigned long long>(grid.x) * block.x;
+        simt::most = simt::most == 0 || grid.y > 65535 ? 0 : std::max(simt::most, row);
+        return hipSuccess;
+    }
     std::mt19937 rng(simt::order_seed);
     simt::body = [&] { kernel(static_cast<P>(a)...); };
     std::vector<unsigned> groups(grid.x);

@@ -30,6 +30,15 @@ extern "C" void grow(unsigned order, int32_t* st, int32_t* fr, int32_t* held, in
     simt::order_seed = order;
     elis::launch_pages_grow(view(st, fr, held, table, scratch, size), slots, lens, cu, n, total, width, blocks, map, nullptr);
 }
+// Threads in a row of the largest launch of a grow of n entries; 0 if there are too many rows.
+extern "C" unsigned long long threads_of(const int32_t* size, int n, int total, int width) {
+    static int32_t some[4];
+    simt::dry = true;
+    simt::most = 1;
+    elis::launch_pages_grow(view(some, some, some, some, some, size), some, some, some, n, total, width, some, some, nullptr);
+    simt::dry = false;
+    return simt::most;
+}
 extern "C" void trim(unsigned order, int32_t* st, int32_t* fr, int32_t* held, int32_t* table, int32_t* scratch, const int32_t* size, const int32_t* slots,
                      const int32_t* lens, int n) {
     simt::order_seed = order;
@@ -101,3 +110,12 @@ def test_pages_in_any_order(lib, n, order):
         lens[gone] = np.minimum(lens[gone], keep)
         assert pool.free[:len(ref.free)].tolist() == ref.free
         assert pool.held.tolist() == [len(h) for h in ref.held] and pool.state[1] == len(ref.free)
+
+
+@pytest.mark.parametrize("n", [129, 1 << 16, (1 << 16) + 1, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, 1 << 27])
+def test_launches_of_many_entries(lib, n):
+    """A row of a launch's grid has fewer than 2^32 threads, however many jobs a call names."""
+    lib.threads_of.restype = ctypes.c_ulonglong
+    size = i32([1 << 20, 16, n, 4])
+    for total, width in ((0, 0), (n, 0), (n, 4), (2 ** 31 - 1, 4)):
+        assert 0 < lib.threads_of(ctypes.c_void_p(size.ctypes.data), n, total, width) < 1 << 32
