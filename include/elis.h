@@ -397,8 +397,10 @@ int elis_pool_head(const elis_weights *w, const float *hidden, const int32_t *cu
  * that stay until the matching init call and are read with elis_read_status
  * on the pool's `state` or the cache's `base`. After a content error the
  * outputs of the entries concerned are undefined; no access leaves the
- * buffers, and the other entries are served. Every call can be captured into
- * a HIP graph.
+ * buffers, and the other entries are served. Offsets that decrease or pass
+ * their total (ELIS_DEV_BAD_CU) concern every entry: they say which rows are
+ * whose, and overlapping ranges may be more work than the call was sized for.
+ * Every call can be captured into a HIP graph.
  */
 
 /*
@@ -510,7 +512,9 @@ size_t elis_kv_attention_workspace_bytes(int32_t n, int32_t total_q, int32_t max
  *  kv_lens     int32 [n].   scale > 0 (times log2(e) still finite).
  *  workspace   256-byte aligned, elis_kv_attention_workspace_bytes() bytes.
  * Products of bf16 operands (the keys and values are exact in bf16, the weights
- * are rounded once) with fp32 sums and statistics. n <= 65535; max_kv <=
+ * are rounded once) with fp32 sums and statistics; weights are at most 2^8 before
+ * they are divided by their sum, so 2^8 times the sum of a column's values should
+ * be below 2^128. n <= 65535; max_kv <=
  * blocks_stride * page_tokens and <= 2^30 (else ELIS_ESHAPE).
  */
 int elis_kv_attention(const elis_kv_cache *c, const uint16_t *q, int64_t q_stride, const int32_t *cu_q, int32_t n,
