@@ -717,15 +717,13 @@ int check_cache_sizes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, 
     return ELIS_OK;
 }
 
-constexpr size_t kKvHeader = 256;
-
 int check_cache(const elis_kv_cache* c) {
     if (!c || !c->base || !aligned(c->base)) return ELIS_EINVAL;
     return check_cache_sizes(c->n_pages, c->page_tokens, c->n_kv_heads, c->d_head);
 }
 
 KvCacheView cache_view(const elis_kv_cache* c) {
-    return KvCacheView{static_cast<uint32_t*>(c->base), static_cast<uint8_t*>(c->base) + kKvHeader,
+    return KvCacheView{static_cast<uint32_t*>(c->base), static_cast<uint8_t*>(c->base) + kCacheHeader,
                        c->n_pages, c->page_tokens, log2_of(c->page_tokens), c->n_kv_heads, c->d_head};
 }
 
@@ -792,7 +790,7 @@ int elis_pages_trim(const elis_page_pool* p, const int32_t* slots, const int32_t
 
 size_t elis_kv_cache_bytes(int32_t n_pages, int32_t page_tokens, int32_t n_kv_heads, int32_t d_head) {
     if (check_cache_sizes(n_pages, page_tokens, n_kv_heads, d_head) != ELIS_OK) return 0;
-    return kKvHeader + static_cast<size_t>(n_pages) * n_kv_heads * (page_tokens / 16) * 17 * d_head;
+    return kCacheHeader + static_cast<size_t>(n_pages) * n_kv_heads * (page_tokens / 16) * 17 * d_head;
 }
 
 int elis_kv_init(const elis_kv_cache* c, void* stream) {

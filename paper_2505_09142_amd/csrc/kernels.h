@@ -172,6 +172,7 @@ hipError_t launch_pages_grow(PagePoolView p, const int32_t* slots, const int32_t
 hipError_t launch_pages_trim(PagePoolView p, const int32_t* slots, const int32_t* lens, int n, hipStream_t st);
 
 // kv_cache.hip: the 4-bit paged cache (records in kv_cache.h).
+constexpr size_t kCacheHeader = 256;  // bytes before a cache's first page: the status word
 struct KvCacheView {
     uint32_t* status;
     uint8_t* pages;

@@ -43,7 +43,7 @@ constexpr int kStep = 32;  // keys a wave takes at a time: two records
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kLowest = -3.0e38f;  // a maximum over no keys: finite, so that differences of maxima are numbers
-constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
+[[maybe_unused]] constexpr int kSpan = 32 * kWaves * kStep;  // keys whose pages the lanes of a work-group hold at a time
 
 // Maxima in single instructions, v_maximum3_f32: fmaxf first quiets each operand's signalling NaN with an instruction of its
 // own (56 more of them for a step of 64 rows). A NaN among the operands is the result. By builtins, because the compiler keeps
@@ -54,7 +54,6 @@ __device__ __forceinline__ float max3(float x, float y, float z) { return max2(m
 // s + both halves of w, a pair of bf16.
 __device__ __forceinline__ float dot2(uint32_t w, float s) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    typedef short s16x2 __attribute__((ext_vector_type(2)));
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), s, false);
 #else
     return s;

@@ -12,8 +12,6 @@
 
 namespace elis {
 
-constexpr size_t kCacheHeader = 256;  // the status word
-
 template <int D>
 struct Rec {
     static constexpr int kGroups = D / 32;
